@@ -39,6 +39,10 @@
  *     one (batch, head); the last one may be shorter.  block_q changes the result, since
  *     each tile selects its own P parents.
  *
+ * Beside the quantized attention stand the exact operators a model needs for the layers, prompts and caches that
+ * stay exact: avq_prompt_attend (packed sequences), avq_cache_append / avq_cache_read / avq_cache_attend (a paged
+ * cache of keys and values, in the tensors' type or in 4 bits).  They have conventions of their own, stated there.
+ *
  * Errors: every entry point validates its arguments on the host and returns a status
  * without launching anything when they are unusable.  Shapes outside the supported
  * envelope give AVQ_ERR_UNSUPPORTED; there is no silent fallback.  Device-side waits on
@@ -93,7 +97,9 @@ enum {
    * that keep every parent's full term (Eq. "correcting_attention").  Equal to the default (masked) form only
    * for codebooks that satisfy parent = mean(children); CUDA-core kernels only (with bfloat16 inputs set
    * AVQ_FLAG_SIMT too: rounding the codebook to bfloat16 already breaks the constraint by an ulp). */
-  AVQ_FLAG_CORRECTING = 4u
+  AVQ_FLAG_CORRECTING = 4u,
+  /* Exact attention (avq_heads) only: a query sees the keys up to its own place. */
+  AVQ_FLAG_CAUSAL = 8u
 };
 
 typedef struct {
@@ -265,6 +271,109 @@ AVQ_API size_t avq_static_workspace_bytes(void);
 AVQ_API avq_status avq_workspace_layout(const avq_problem* prob, int32_t P, int32_t block_q,
                                 size_t* parent_idx_off, size_t* child_idx_off, size_t* Vp_off,
                                 size_t* np_off, size_t* Vc_off, size_t* nc_off);
+
+/* ======================================================================== exact attention
+ * The ordinary softmax attention that the quantized one approximates, for serving: packed prompts of different
+ * lengths, and a paged cache of keys and values that is appended to and attended over.  Query heads may share key
+ * heads: query head h reads key head h / (H / Hk).
+ *
+ * Rows are tokens.  A tensor of T rows and n heads is [T, n, d] with the heads of a row dense; consecutive rows lie
+ * `stride` elements apart, so that Q, K and V may be views of one projection's output.  Strides are at least n*d and,
+ * like the pointers, multiples of 16 bytes.  Heads, lengths and tables as int32; sums, softmax statistics and `lse` in
+ * float32.  A query that sees no key gives a row of zeros and lse = -inf.
+ *
+ * Header: 256 bytes of device memory, 256-byte aligned, that the CALLER ZEROES ONCE before its first use; kernels record
+ * there what they had to skip or gave up (avq_check() reports and clears it).  A call reads no other contents of a
+ * workspace than those it has written itself.
+ */
+typedef struct {
+  int32_t H, Hk;       /* query heads; key and value heads, a divisor of H                */
+  int32_t d;           /* head dimension                                                  */
+  int32_t dtype;       /* avq_dtype of Q, K, V, Y                                         */
+  float scale;         /* logits are scale * <q, k>                                       */
+  uint32_t flags;      /* AVQ_FLAG_CAUSAL (avq_prompt_attend), AVQ_FLAG_SIMT              */
+} avq_heads;
+
+/* Envelope of the exact operators.
+ *   CUDA-core kernels (AVQ_FLAG_SIMT; float32 prompts always): d % 8 == 0, 8 <= d <= 256, any finite scale.
+ *   Tensor-core kernels: d in {64, 128}, scale > 0; avq_prompt_attend (bfloat16): H / Hk <= 128.
+ *   Caches: page a multiple of 16, 16..1024; pages * page < 2^31; in 4 bits d % 32 == 0.
+ */
+
+/* Attention of S packed sequences.  Sequence s has the queries cu_q[s] .. cu_q[s+1]-1 and the keys cu_k[s] ..
+ * cu_k[s+1]-1 (device int32 [S+1], nondecreasing; cu_k NULL: the same as cu_q).  Every query sees all keys of its
+ * sequence, with AVQ_FLAG_CAUSAL query i of nq the keys j <= i + nk - nq (the queries are the last ones of the keys).
+ *   Q [Tq,H,d]   K, V [Tk,Hk,d]   Y [Tq,H,d]   lse_out: optional float32 [Tq,H], log sum_j exp(scale <q,k_j>)
+ *   workspace    avq_prompt_workspace_bytes() bytes: the header.
+ * Rows of Y (and lse_out) that belong to no sequence stay as they were.  Keys a query does not see have no effect on
+ * its row, whatever they and their values hold, infinities and NaN included.  A sequence whose bounds are not
+ * 0 <= cu[s] <= cu[s+1] <= T is left out and reported by avq_check() as AVQ_ERR_INDEX.  A call with S or Tq of 0
+ * launches nothing. */
+AVQ_API size_t avq_prompt_workspace_bytes(const avq_heads* heads);
+AVQ_API avq_status avq_prompt_attend(const avq_heads* heads, const void* Q, int64_t q_stride, const void* K,
+                             int64_t k_stride, const void* V, int64_t v_stride, const int32_t* cu_q,
+                             const int32_t* cu_k, int32_t S, int32_t Tq, int32_t Tk, void* Y, int64_t y_stride,
+                             float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* A paged cache of keys and values.  Page p, head h starts at element (p * Hk + h) * page * d of `keys` and `values`
+ * and holds `page` rows of d elements of `dtype` (bits: that type's width), or, with bits = 4, at byte
+ * (p * Hk + h) * page * 5d/8:
+ *     page rows of d/2 bytes: codes 0..15, two to a byte; the codes of dimensions 32 g + 8 t .. + 7 fill, lowest
+ *       first, the 4 bytes at t * d/8 + 4 g (t < 4, g < d/32);
+ *     page rows of d/8 bytes: for each group g of 32 dimensions the bfloat16 pair (lo_g, step_g).
+ * A code c stands for lo_g + c * step_g.  Of a group's values x, lo is the smallest and step a fifteenth of the
+ * largest less lo, each rounded to bfloat16, and c = (x - lo) / step rounded to nearest even, within 0..15 (0 where
+ * step is 0).  A group with an infinity or a NaN reads as NaN.
+ * Slot s is row s % page of page s / page. */
+typedef struct {
+  void *keys, *values;
+  int32_t pages, page; /* number of pages, rows of a page                                 */
+  int32_t Hk, d;
+  int32_t dtype;       /* avq_dtype of the rows that go in and come out                   */
+  int32_t bits;        /* 32 (float32), 16 (bfloat16) or 4                                */
+} avq_cache;
+
+/* Rotation by position: a pair (x1, x2) becomes (x1 cos - x2 sin, x2 cos + x1 sin), in float32, rounded once to dtype.
+ * cos, sin: float32 [rows, dims/2]; pair k of the token at position pos[i] takes entry [pos[i], k].  Pair k is
+ * dimensions (k, k + dims/2), or (2k, 2k+1) where `adjacent` is set; dimensions from dims on stay.  dims % 16 == 0. */
+typedef struct {
+  const float *cos, *sin;
+  const int32_t* pos;  /* device int32 [T]                                                */
+  int32_t rows, dims, adjacent;
+} avq_rotation;
+
+/* Bytes of `keys` (and of `values`); 0 if the description is invalid.  Host function; ignores the pointers. */
+AVQ_API size_t avq_cache_bytes(const avq_cache* cache);
+
+/* Stores T rows of keys, rotated if `rot` is given, and of values at slots[i] (device int32 [T]).  With Q, the same
+ * tokens' queries [T,H,d], Q_out gets them rotated (Q_out may be Q, with the same stride; without `rot` they are
+ * copied).  A token with slot -1 is skipped, its row of Q_out left as it was; one whose slot or position is out of
+ * range is skipped and reported by avq_check(header) as AVQ_ERR_INDEX.  Slots other than -1 must differ from each
+ * other: of a slot named twice the contents are unspecified.  header may be NULL (nothing is reported then). */
+AVQ_API avq_status avq_cache_append(const avq_cache* cache, const void* K, int64_t k_stride, const void* V, int64_t v_stride,
+                            const int32_t* slots, int32_t T, const avq_rotation* rot, const void* Q,
+                            int64_t q_stride, int32_t H, void* Q_out, int64_t q_out_stride, void* header,
+                            void* stream);
+
+/* Rows of the cache back as [T,Hk,d] of dtype: rows i of K and V get slot slots[i] (any may repeat); -1 and slots out
+ * of range leave their rows as they were, the latter reported. */
+AVQ_API avq_status avq_cache_read(const avq_cache* cache, const int32_t* slots, int32_t T, void* K, int64_t k_stride, void* V,
+                          int64_t v_stride, void* header, void* stream);
+
+/* The last nq queries of B sequences over their cached keys, theirs among them: sequence b has lens[b] tokens in the
+ * pages table[b, 0 .. ceil(lens[b] / page) - 1] (device int32 [B, table_pages]); its query i sees the tokens
+ * j <= lens[b] - nq + i.
+ *   Q, Y [B*nq,H,d] (row b*nq + i)   lse_out: optional float32 [B*nq,H]
+ *   workspace: avq_cache_attend_workspace_bytes() bytes, 256-byte aligned, its first 256 the header.
+ * flags: AVQ_FLAG_SIMT only.  Tokens a query does not see have no effect on its row.  A length outside
+ * 0 .. table_pages * page counts as the nearer of the two, the tokens of a page outside 0 .. pages-1 are left out, and
+ * both are reported by avq_check() as AVQ_ERR_INDEX.  Results do not depend on what else runs: partial sums of long
+ * sequences are joined in a fixed order.  Calls that may overlap need workspaces of their own. */
+AVQ_API size_t avq_cache_attend_workspace_bytes(const avq_heads* heads, int32_t B, int32_t nq);
+AVQ_API avq_status avq_cache_attend(const avq_heads* heads, const avq_cache* cache, const void* Q, int64_t q_stride,
+                            const int32_t* table, int32_t table_pages, const int32_t* lens, int32_t B, int32_t nq,
+                            void* Y, int64_t y_stride, float* lse_out, void* workspace, size_t workspace_bytes,
+                            void* stream);
 
 /* Waits for `stream`, reads the status word in the workspace header and clears it.
  * AVQ_OK, AVQ_ERR_DEVICE_TIMEOUT (a bounded wait inside a kernel expired; outputs of that

@@ -16,7 +16,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "lib", "libavq_attn.so")
 
 AVQ_F32, AVQ_BF16 = 0, 1
-FLAG_PARENT_STAYS, FLAG_SIMT, FLAG_CORRECTING = 1, 2, 4
+FLAG_PARENT_STAYS, FLAG_SIMT, FLAG_CORRECTING, FLAG_CAUSAL = 1, 2, 4, 8
 STATUS_NAMES = {0: "AVQ_OK", 1: "AVQ_ERR_NULL", 2: "AVQ_ERR_SHAPE", 3: "AVQ_ERR_UNSUPPORTED", 4: "AVQ_ERR_ALIGN",
                 5: "AVQ_ERR_WORKSPACE", 6: "AVQ_ERR_CUDA", 7: "AVQ_ERR_DEVICE_TIMEOUT", 8: "AVQ_ERR_INDEX"}
 
@@ -24,13 +24,30 @@ EXPORTS = ("avq_workspace_bytes", "avq_assign", "avq_aggregate", "avq_forward", 
            "avq_workspace_layout", "avq_check", "avq_status_string", "avq_version", "avq_forward_static",
            "avq_check_static", "avq_static_workspace_bytes", "avq_workspace_bytes_permuted",
            "avq_forward_permuted", "avq_codebook_update_workspace_bytes", "avq_codebook_update",
-           "avq_forward_tiled")
+           "avq_forward_tiled", "avq_prompt_workspace_bytes", "avq_prompt_attend", "avq_cache_bytes", "avq_cache_append",
+           "avq_cache_read", "avq_cache_attend_workspace_bytes", "avq_cache_attend")
 
 
 class AvqProblem(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("Nq", ctypes.c_int32), ("Nk", ctypes.c_int32),
                 ("d", ctypes.c_int32), ("M", ctypes.c_int32), ("C", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class AvqHeads(ctypes.Structure):
+    _fields_ = [("H", ctypes.c_int32), ("Hk", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class AvqCache(ctypes.Structure):
+    _fields_ = [("keys", ctypes.c_void_p), ("values", ctypes.c_void_p), ("pages", ctypes.c_int32),
+                ("page", ctypes.c_int32), ("Hk", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("bits", ctypes.c_int32)]
+
+
+class AvqRotation(ctypes.Structure):
+    _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("pos", ctypes.c_void_p),
+                ("rows", ctypes.c_int32), ("dims", ctypes.c_int32), ("adjacent", ctypes.c_int32)]
 
 
 class AvqError(RuntimeError):
@@ -78,6 +95,19 @@ def lib() -> ctypes.CDLL:
         L.avq_codebook_update_workspace_bytes.restype, L.avq_codebook_update_workspace_bytes.argtypes = sz, [pp]
         L.avq_codebook_update.restype = i32
         L.avq_codebook_update.argtypes = [pp, vp, vp, vp, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        i64, ph, pc = ctypes.c_int64, ctypes.POINTER(AvqHeads), ctypes.POINTER(AvqCache)
+        L.avq_prompt_workspace_bytes.restype, L.avq_prompt_workspace_bytes.argtypes = sz, [ph]
+        L.avq_prompt_attend.restype = i32
+        L.avq_prompt_attend.argtypes = [ph, vp, i64, vp, i64, vp, i64, vp, vp, i32, i32, i32, vp, i64, vp, vp, sz, vp]
+        L.avq_cache_bytes.restype, L.avq_cache_bytes.argtypes = sz, [pc]
+        L.avq_cache_append.restype = i32
+        L.avq_cache_append.argtypes = [pc, vp, i64, vp, i64, vp, i32, ctypes.POINTER(AvqRotation), vp, i64, i32, vp,
+                                       i64, vp, vp]
+        L.avq_cache_read.restype, L.avq_cache_read.argtypes = i32, [pc, vp, i32, vp, i64, vp, i64, vp, vp]
+        L.avq_cache_attend_workspace_bytes.restype = sz
+        L.avq_cache_attend_workspace_bytes.argtypes = [ph, i32, i32]
+        L.avq_cache_attend.restype = i32
+        L.avq_cache_attend.argtypes = [ph, pc, vp, i64, vp, i32, vp, i32, i32, vp, i64, vp, vp, sz, vp]
         L.avq_status_string.restype, L.avq_status_string.argtypes = ctypes.c_char_p, [i32]
         L.avq_version.restype, L.avq_version.argtypes = i32, []
         _lib = L
@@ -329,3 +359,211 @@ def forward_static(Q, K, V, Cp, Cc, P: int, block_q: int, scale=None, flags: int
     if st != 0:
         raise AvqError(st, "avq_check_static")
     return (Y, topp, imp) if aux else Y
+
+
+# ---------------------------------------------------------------- exact attention
+def _rows(name, t, heads, d, dtype, T=None):
+    """A tensor of T rows, [T, heads, d] with dense heads and rows any distance apart; returns that distance."""
+    if t.dim() != 3 or tuple(t.shape[1:]) != (heads, d) or (T is not None and t.shape[0] != T):
+        raise ValueError(f"{name} must be [{'T' if T is None else T}, {heads}, {d}], not {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.shape[0] and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != d)):
+        raise ValueError(f"the heads of a row of {name} must be dense")
+    # (the stride of a single row, or of none, is anybody's: any usable one will do)
+    return t.stride(0) if t.shape[0] > 1 else heads * d
+
+
+def _ints(name, t, *shape):
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape}, not {t.dtype} {tuple(t.shape)}")
+
+
+def _here(**ts):
+    """All tensors are on the current CUDA device, whose current stream the call goes to."""
+    at = None
+    for name, t in ts.items():
+        if t is None:
+            continue
+        if t.is_cuda and at is None:
+            at = torch._C._cuda_getDevice()
+        if not t.is_cuda or t.get_device() != at:
+            raise ValueError(f"{name} must be on the current CUDA device, not {t.device}")
+
+
+def _addr(t):
+    return 0 if t is None else t.data_ptr()
+
+
+class ExactAttention:
+    """avq_prompt_attend: softmax attention over packed sequences, planned for one set of heads.
+
+    ``ExactAttention(H, Hk, d)(Q, K, V, cu_q, cu_k=None)`` takes Q [Tq,H,d], K, V [Tk,Hk,d] (rows may be views of a
+    wider tensor) and the int32 bounds [S+1] of the sequences' queries and keys, and returns Y [Tq,H,d], with ``lse`` also
+    the log of every query's sum, float32 [Tq,H].  Rows outside all sequences are left as they are (in a Y made here: anything)."""
+
+    def __init__(self, H, Hk, d, dtype=torch.bfloat16, scale=None, causal=True, flags=0, device="cuda"):
+        code = {torch.float32: AVQ_F32, torch.bfloat16: AVQ_BF16}.get(dtype)
+        if code is None:
+            raise TypeError(f"unsupported dtype {dtype}")
+        self.heads = AvqHeads(H, Hk, d, code, float(scale) if scale is not None else 1.0 / math.sqrt(d),
+                              flags | (FLAG_CAUSAL if causal else 0))
+        self.dtype = dtype
+        n = int(lib().avq_prompt_workspace_bytes(self.heads))
+        if n == 0:
+            raise AvqError(lib().avq_prompt_attend(self.heads, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0) or 3,
+                           "avq_prompt_workspace_bytes")
+        self.workspace = torch.zeros(n, dtype=torch.uint8, device=device)
+
+    def __call__(self, Q, K, V, cu_q, cu_k=None, Y=None, lse=False):
+        h = self.heads
+        Tq, Tk, S = Q.shape[0], K.shape[0], cu_q.shape[0] - 1
+        qs, ks, vs = (_rows("Q", Q, h.H, h.d, self.dtype), _rows("K", K, h.Hk, h.d, self.dtype),
+                      _rows("V", V, h.Hk, h.d, self.dtype, Tk))
+        if S < 0 or (cu_k is None and Tq != Tk):
+            raise ValueError("cu_q must hold S + 1 bounds, and cu_k too where queries and keys differ in number")
+        _ints("cu_q", cu_q, S + 1)
+        if cu_k is not None:
+            _ints("cu_k", cu_k, S + 1)
+        _here(Q=Q, K=K, V=V, cu_q=cu_q, cu_k=cu_k, Y=Y, workspace=self.workspace)
+        if Y is None:
+            Y = torch.empty((Tq, h.H, h.d), dtype=self.dtype, device=Q.device)
+        ys = _rows("Y", Y, h.H, h.d, self.dtype, Tq)
+        L = torch.empty((Tq, h.H), dtype=torch.float32, device=Q.device) if lse else None
+        st = (_lib or lib()).avq_prompt_attend(h, _addr(Q), qs, _addr(K), ks, _addr(V), vs, _addr(cu_q), _addr(cu_k), S, Tq,
+                                               Tk, _addr(Y), ys, _addr(L), self.workspace.data_ptr(),
+                                               self.workspace.numel(), _raw_stream())
+        if st != 0:
+            raise AvqError(st, "avq_prompt_attend")
+        return (Y, L) if lse else Y
+
+    def check(self) -> None:
+        """avq_check: raises if a kernel left something out (unusable bounds) or gave up on a wait."""
+        st = lib().avq_check(_ptr(self.workspace), _stream())
+        if st != 0:
+            raise AvqError(st, "avq_check")
+
+
+class PagedCache:
+    """A paged cache of keys and values over the caller's two buffers (avq_cache): ``append``, ``read``, ``attend``.
+
+    ``bits``: the width of ``dtype`` for rows of that type, buffers [pages, Hk, page, d]; 4 for groups of 32 dimensions in
+    4 bits, buffers uint8 [pages, Hk, page * 5 d / 8].  ``PagedCache.empty`` makes the buffers."""
+
+    def __init__(self, keys, values, page, d, dtype=torch.bfloat16, bits=None):
+        code = {torch.float32: AVQ_F32, torch.bfloat16: AVQ_BF16}.get(dtype)
+        if code is None:
+            raise TypeError(f"unsupported dtype {dtype}")
+        width = 32 if code == AVQ_F32 else 16
+        bits = width if bits is None else bits
+        pages, Hk = keys.shape[:2]
+        want = ((pages, Hk, page * 5 * d // 8), torch.uint8) if bits == 4 else ((pages, Hk, page, d), dtype)
+        for name, t in (("keys", keys), ("values", values)):
+            if (tuple(t.shape), t.dtype) != want or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous {want[1]} {want[0]}, not {t.dtype} {tuple(t.shape)}")
+        self.keys, self.values, self.dtype = keys, values, dtype
+        self.desc = AvqCache(keys.data_ptr(), values.data_ptr(), pages, page, Hk, d, code, bits)
+        if int(lib().avq_cache_bytes(self.desc)) == 0:
+            raise AvqError(lib().avq_cache_read(self.desc, 0, 0, 0, 0, 0, 0, 0, 0) or 3, "avq_cache_bytes")
+        self.header = torch.zeros(256, dtype=torch.uint8, device=keys.device)
+
+    @classmethod
+    def empty(cls, pages, page, Hk, d, dtype=torch.bfloat16, bits=None, device="cuda"):
+        shape, dt = ((pages, Hk, page * 5 * d // 8), torch.uint8) if bits == 4 else ((pages, Hk, page, d), dtype)
+        return cls(torch.zeros(shape, dtype=dt, device=device), torch.zeros(shape, dtype=dt, device=device), page, d, dtype, bits)
+
+    def append(self, K, V, slots, pos=None, cos=None, sin=None, adjacent=False, Q=None, Q_out=None):
+        """avq_cache_append: K, V [T,Hk,d] to the rows ``slots`` (int32 [T], -1: none), K rotated by the positions ``pos``
+        (int32 [T]) with the float32 tables ``cos``, ``sin`` [rows, dims/2].  With Q [T,H,d] returns the rotated queries (in a
+        Q_out made here the rows of slot -1 are anything)."""
+        c = self.desc
+        T = K.shape[0]
+        ks, vs = _rows("K", K, c.Hk, c.d, self.dtype), _rows("V", V, c.Hk, c.d, self.dtype, T)
+        _ints("slots", slots, T)
+        rot = None
+        if pos is not None:
+            _ints("pos", pos, T)
+            for name, t in (("cos", cos), ("sin", sin)):
+                if t is None or t.dtype != torch.float32 or t.dim() != 2 or not t.is_contiguous() or t.shape != cos.shape:
+                    raise ValueError(f"{name} must be a contiguous float32 table [rows, dims/2]")
+            rot = AvqRotation(cos.data_ptr(), sin.data_ptr(), pos.data_ptr(), cos.shape[0], 2 * cos.shape[1], int(adjacent))
+        elif cos is not None or sin is not None:
+            raise ValueError("a rotation needs the positions")
+        H = qs = os_ = 0
+        if Q is not None:
+            H = Q.shape[1]
+            qs = _rows("Q", Q, H, c.d, self.dtype, T)
+            if Q_out is None:
+                Q_out = torch.empty((T, H, c.d), dtype=self.dtype, device=Q.device)
+            os_ = _rows("Q_out", Q_out, H, c.d, self.dtype, T)
+        elif Q_out is not None:
+            raise ValueError("Q_out without Q")
+        _here(K=K, V=V, slots=slots, pos=pos, cos=cos, sin=sin, Q=Q, Q_out=Q_out, keys=self.keys)
+        st = (_lib or lib()).avq_cache_append(c, _addr(K), ks, _addr(V), vs, _addr(slots), T, rot, _addr(Q), qs, H,
+                                              _addr(Q_out), os_, self.header.data_ptr(), _raw_stream())
+        if st != 0:
+            raise AvqError(st, "avq_cache_append")
+        return Q_out
+
+    def read(self, slots, K=None, V=None):
+        """avq_cache_read: the rows ``slots`` back as (K, V) [T,Hk,d]; rows of -1 are left as they are (in tensors
+        made here: anything)."""
+        c = self.desc
+        T = slots.shape[0]
+        _ints("slots", slots, T)
+        if K is None:
+            K = torch.empty((T, c.Hk, c.d), dtype=self.dtype, device=slots.device)
+        if V is None:
+            V = torch.empty((T, c.Hk, c.d), dtype=self.dtype, device=slots.device)
+        ks, vs = _rows("K", K, c.Hk, c.d, self.dtype, T), _rows("V", V, c.Hk, c.d, self.dtype, T)
+        _here(slots=slots, K=K, V=V, keys=self.keys)
+        st = (_lib or lib()).avq_cache_read(c, _addr(slots), T, _addr(K), ks, _addr(V), vs, self.header.data_ptr(),
+                                            _raw_stream())
+        if st != 0:
+            raise AvqError(st, "avq_cache_read")
+        return K, V
+
+    def plan(self, H, B, nq=1, scale=None, flags=0):
+        """Workspace and heads of repeated ``attend`` calls of B sequences with nq queries each."""
+        c = self.desc
+        heads = AvqHeads(H, c.Hk, c.d, c.dtype, float(scale) if scale is not None else 1.0 / math.sqrt(c.d), flags)
+        n = int(lib().avq_cache_attend_workspace_bytes(heads, B, nq))
+        if n == 0:
+            raise AvqError(lib().avq_cache_attend(heads, c, 0, 0, 0, 0, 0, B, nq, 0, 0, 0, 0, 0, 0) or 3,
+                           "avq_cache_attend_workspace_bytes")
+        ws = torch.empty(n, dtype=torch.uint8, device=self.keys.device)
+        ws[:256].zero_()
+        return heads, ws, B, nq
+
+    def attend(self, Q, table, lens, scale=None, flags=0, Y=None, lse=False, plan=None):
+        """avq_cache_attend: the last queries Q [B*nq,H,d] of B sequences (``lens`` int32 [B] tokens in the pages ``table``
+        int32 [B, n]) over the cache.  Returns Y, or (Y, lse).  ``plan``: what ``plan`` made, else one is made here."""
+        c = self.desc
+        B = lens.shape[0]
+        if plan is None:
+            if B == 0 or Q.shape[0] % B:
+                raise ValueError("Q must hold the same number of rows for each of the sequences of lens")
+            plan = self.plan(Q.shape[1], B, max(1, Q.shape[0] // B), scale, flags)
+        heads, ws, pB, nq = plan
+        if B != pB or table.dim() != 2:
+            raise ValueError(f"lens must be [{pB}] and table [{pB}, n]")
+        qs = _rows("Q", Q, heads.H, c.d, self.dtype, B * nq)
+        _ints("lens", lens, B)
+        _ints("table", table, B, table.shape[1])
+        if Y is None:
+            Y = torch.empty((B * nq, heads.H, c.d), dtype=self.dtype, device=Q.device)
+        ys = _rows("Y", Y, heads.H, c.d, self.dtype, B * nq)
+        _here(Q=Q, table=table, lens=lens, Y=Y, keys=self.keys, workspace=ws)
+        L = torch.empty((B * nq, heads.H), dtype=torch.float32, device=Q.device) if lse else None
+        st = (_lib or lib()).avq_cache_attend(heads, c, _addr(Q), qs, _addr(table), table.shape[1], _addr(lens), B, nq,
+                                              _addr(Y), ys, _addr(L), ws.data_ptr(), ws.numel(), _raw_stream())
+        if st != 0:
+            raise AvqError(st, "avq_cache_attend")
+        return (Y, L) if lse else Y
+
+    def check(self, plan=None) -> None:
+        """avq_check of the cache's header, or of a plan's: raises if a kernel skipped a slot, position, length or page
+        out of range."""
+        st = lib().avq_check(_ptr(self.header if plan is None else plan[1]), _stream())
+        if st != 0:
+            raise AvqError(st, "avq_check")
