@@ -1,5 +1,5 @@
 // C ABI of the exact operators: argument validation and dispatch.  The kernels live in avq_exact_simt.cu (CUDA cores,
-// and the joining of split sequences) and avq_cache.cu (rows into and out of a cache).
+// and the joining of split sequences), avq_tc_cached.cu (tensor cores) and avq_cache.cu (rows into and out of a cache).
 #include "avq_exact.cuh"
 
 namespace avq {
@@ -179,7 +179,7 @@ avq_status avq_cache_attend(const avq_heads* heads, const avq_cache* cache, cons
                         table, lens, q_stride, y_stride, h.H, h.Hk, h.d, B, nq, c.pages, c.page, table_pages, h.scale,
                         static_cast<int32_t*>(workspace)};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return simt_cached(a, h.dtype, c.bits, st);
+  return tensor_path(h) ? tc_cached(a, h.dtype, c.bits, st) : simt_cached(a, h.dtype, c.bits, st);
 }
 
 }  // extern "C"

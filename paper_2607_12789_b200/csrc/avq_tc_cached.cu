@@ -1,0 +1,708 @@
+// Attention over a paged cache on the tensor cores (d 64 or 128): rows of bfloat16, rows of float32, or 4 bits.
+//
+// One query has a product of d multiply-adds with every cached token, so the call is bound by reading the cache once; the
+// arithmetic has to keep out of the way.  Query heads that share a key head, and the nq queries of a sequence, are the
+// rows of one product: S^T = K Q^T with 16 tokens by 8 (NT = 1) or 16 (NT = 2) rows, O^T += V^T P^T, by warp-level
+// mma.sync (the rows are too few for tcgen05's 128 x N tiles, and both operands of the second product come from where
+// they are: values from shared memory, weights from registers).
+//
+// The units of all segments are dealt out evenly (avq_exact.cuh).  Each warp of a CTA takes every kWarps-th unit of 16
+// tokens through a ring of its own in shared memory, filled by 16-byte cp.async STAGES - 1 units ahead, with running
+// maxima, sums and output of its own: no barrier between warps until a segment's end, when they are added in the order
+// of the warps.  Chunks of 16 bytes are swizzled so that every fragment load is free of bank conflicts.
+//
+// 4 bits: the codes enter the products as integers and are never turned into the values they stand for.
+//   keys    s = sum_g step_g <q_g, c_g> + lo_g sum(q_g):  one accumulator per group of 32 dimensions.
+//   values  o_g += (p step_g) c + (p lo_g):  the weight is multiplied by each group's step before it is rounded to
+//           bfloat16; p lo_g is summed per row and group in float32.
+//   A pair of codes becomes a pair of bfloat16 by one AND-OR: 0x4300 | c is 128 + c.  The 128 is taken out again: of s
+//   with lo_g - 128 step_g in the place of lo_g, of o by a product of the same rounded weights with a constant -128, so
+//   that nothing of a rounding is left behind.
+// float32: rows by tf32 products of two parts each (the lowest product left out: 2^-22 of a term); 4 bits with float32
+// queries by three bfloat16 parts of the query and of the weight, which are all of their 24 bits.
+//
+// The running maximum of a row is raised only when a logit exceeds it by 2^8 (weights stay below 2^8, sums far inside
+// float32): most units need a vote instead of shuffles and rescaling.
+#include "avq_exact.cuh"
+#include "avq_tc_common.cuh"
+
+namespace avq {
+namespace exact {
+namespace {
+
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr float kRaise = 8.f;
+enum Rows { kBf16 = 0, kQ4 = 1, kF32 = 2 };
+
+template <int MODE, int D> __host__ __device__ constexpr int unit_bytes() {
+  return MODE == kQ4 ? 2 * kUnit * (D / 2 + D / 8) : 2 * kUnit * D * (MODE == kF32 ? 4 : 2);
+}
+template <int MODE, int D> __host__ __device__ constexpr int stages() { return MODE == kQ4 ? 6 : MODE == kBf16 && D == 64 ? 5 : 3; }
+template <int MODE, int D, int NT> __host__ __device__ constexpr int ctas_per_sm() { return MODE == kQ4 && NT == 1 ? 3 : MODE == kF32 && D == 128 ? 1 : 2; }
+// Query fragments in shared memory: float32 queries only (their parts would take too many registers).
+template <int MODE, int D, int NT, int PARTS> __host__ __device__ constexpr int query_bytes() {
+  return MODE == kF32 ? (D / 8) * NT * 32 * 16 : MODE == kQ4 && PARTS == 3 ? (D / 16) * NT * 32 * 24 : 0;
+}
+template <int MODE, int D, int NT, int PARTS> __host__ __device__ constexpr size_t cached_smem() {
+  return (size_t)kWarps * stages<MODE, D>() * unit_bytes<MODE, D>() + query_bytes<MODE, D, NT, PARTS>();
+}
+
+__device__ __forceinline__ uint32_t swizzle(int r) { return ((r & 1) << 2) | (r & 2) | ((r >> 2) & 1); }
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {   // the rest of 16 bytes: zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {   // an 8 x 8 matrix of 16-bit values, a pair per lane
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  return v;
+}
+template <int N> __device__ __forceinline__ void lds_words(uint32_t (&w)[N], uint32_t at) {   // N = 2 or 4
+  if constexpr (N == 4) {
+    const uint4 v = lds128(at);
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+  } else {
+    const uint2 v = lds64(at);
+    w[0] = v.x; w[1] = v.y;
+  }
+}
+// 128 + c of the codes at bits 4 i of both halves
+__device__ __forceinline__ uint32_t codes_at(uint32_t w, int i) { return ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u; }
+__device__ __forceinline__ float tf32_high(float x) { return __uint_as_float(__float_as_uint(x) & 0xffffe000u); }
+__device__ __forceinline__ float low_f(uint32_t pair) { return __uint_as_float(pair << 16); }
+__device__ __forceinline__ float high_f(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
+// Three bfloat16 parts of a pair of float32 values, which add up to them exactly (but for values near the smallest).
+__device__ __forceinline__ void three_parts(float x, float y, uint32_t (&p)[3]) {
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    p[i] = pack_bf16(x, y);
+    x -= low_f(p[i]);
+    y -= high_f(p[i]);
+  }
+}
+
+template <int MODE, int D, int NT, int PARTS>
+struct Warp {
+  [[maybe_unused]] static constexpr int kChunks = D * (MODE == kF32 ? 4 : 2) / 16;          // of a raw row
+  static constexpr int kGroups = D / 32;
+  static constexpr int kUnitBytes = unit_bytes<MODE, D>();
+  static constexpr int kV = MODE == kQ4 ? kUnit * D / 2 : kUnitBytes / 2;  // offsets within a unit
+  [[maybe_unused]] static constexpr int kKPairs = kUnit * D, kVPairs = kKPairs + kUnit * D / 8;
+
+  float O[D / 16][NT][4];        // C fragments of O^T: columns (rows of the product) 8 nt + 2 t, + 1
+  float m[NT][2], l[NT][2];      // maximum (the same in the 8 lanes of a column), this lane's share of the sum
+  float off[NT][2][MODE == kQ4 ? kGroups : 1];   // sum p lo_g, this lane's share
+  uint32_t q[MODE == kBf16 || (MODE == kQ4 && PARTS == 1) ? D / 16 : 1][NT][2];
+  float qsum[MODE == kQ4 ? kGroups : 1][NT][2];
+  int lim[NT][2];                // tokens that the column's query sees
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) O[i][n][e] = 0.f;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        m[n][e] = -INFINITY;
+        l[n][e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < (MODE == kQ4 ? kGroups : 1); ++w) off[n][e][w] = 0.f;
+      }
+  }
+
+  // Copies of one unit's rows into `dst` (shared), `rows` of them (0: none, zeros instead).
+  static __device__ __forceinline__ void fetch(uint32_t dst, const CachedArgs& a, int page, int hk, int row0, int rows, int lane) {
+    const int64_t head = (int64_t)max(page, 0) * a.Hk + hk;
+    if (page < 0) rows = 0;
+    if constexpr (MODE == kQ4) {
+      const char* k = static_cast<const char*>(a.keys) + head * q4_page_bytes(a.page, D);
+      const char* v = static_cast<const char*>(a.values) + head * q4_page_bytes(a.page, D);
+      constexpr int per = D / 32, count = kUnit * per;   // 16-byte chunks of a code row, of the unit
+#pragma unroll
+      for (int i0 = 0; i0 < count; i0 += 32) {
+        const int i = i0 + lane, r = i / per, c = i % per;
+        const uint32_t at = dst + 16 * (r * per + (D == 128 ? c ^ ((r >> 1) & 3) : c ^ ((r >> 2) & 1)));
+        const int n = r < rows ? 16 : 0;
+        cp_async16(at, k + row0 * (D / 2) + 16 * i, n);
+        cp_async16(at + kV, v + row0 * (D / 2) + 16 * i, n);
+      }
+      constexpr int pairs = kUnit * D / 8 / 16;          // chunks of (lo, step) pairs: 16 or 8
+      if (lane < 2 * pairs) {
+        const int i = lane % pairs;
+        const char* src = (lane < pairs ? k : v) + a.page * (D / 2) + row0 * (D / 8) + 16 * i;
+        const int n = min(16, max(0, rows * (D / 8) - 16 * i));
+        cp_async16(dst + (lane < pairs ? kKPairs : kVPairs) + 16 * i, src, n);
+      }
+    } else {
+      constexpr int row = kChunks * 16;
+      const char* k = static_cast<const char*>(a.keys) + (head * a.page + row0) * row;
+      const char* v = static_cast<const char*>(a.values) + (head * a.page + row0) * row;
+#pragma unroll 8
+      for (int i0 = 0; i0 < kUnit * kChunks; i0 += 32) {
+        const int i = i0 + lane, r = i / kChunks, c = i % kChunks;
+        const uint32_t at = dst + r * row + 16 * (c ^ swizzle(r));
+        const int n = r < rows ? 16 : 0;
+        cp_async16(at, k + 16 * i, n);
+        cp_async16(at + kV, v + 16 * i, n);
+      }
+    }
+  }
+
+  // The queries of a segment: fragments in registers, or (float32) written to shared memory by one warp for all.
+  template <typename T>
+  __device__ __forceinline__ void load_queries(const CachedArgs& a, const Segment& sg, uint4* shared, bool write, int lane) {
+    const int g = lane >> 2, t = lane & 3, G = a.H / a.Hk, rows = min(kRows, a.nq * G - sg.block * kRows);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int r = 8 * n + g, qi = sg.block * kRows + r;
+      const bool ok = r < rows;
+      const T* src = static_cast<const T*>(a.Q) + ((int64_t)sg.b * a.nq + (ok ? qi / G : 0)) * a.q_stride +
+                     ((int64_t)sg.hk * G + (ok ? qi % G : 0)) * D;
+      auto at = [&](int k) { return ok ? to_f32(src[k]) : 0.f; };
+      if constexpr (MODE == kBf16) {
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          q[k][n][0] = ok ? *reinterpret_cast<const uint32_t*>(src + 16 * k + 2 * t) : 0u;
+          q[k][n][1] = ok ? *reinterpret_cast<const uint32_t*>(src + 16 * k + 2 * t + 8) : 0u;
+        }
+      } else if constexpr (MODE == kQ4) {
+        float part[kGroups];
+#pragma unroll
+        for (int w = 0; w < kGroups; ++w) {
+          float x[8];
+          if (ok) load8(src + 32 * w + 8 * t, x);
+          else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = 0.f;
+          }
+          part[w] = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            if constexpr (PARTS == 1) {
+              q[2 * w + s][n][0] = pack_bf16(x[2 * s], x[2 * s + 4]);
+              q[2 * w + s][n][1] = pack_bf16(x[2 * s + 1], x[2 * s + 5]);
+            } else if (write) {
+              uint32_t p0[3], p1[3];
+              three_parts(x[2 * s], x[2 * s + 4], p0);
+              three_parts(x[2 * s + 1], x[2 * s + 5], p1);
+              uint2* to = reinterpret_cast<uint2*>(shared) + ((2 * w + s) * NT + n) * 3 * 32 + lane;
+#pragma unroll
+              for (int i = 0; i < 3; ++i) to[32 * i] = make_uint2(p0[i], p1[i]);
+            }
+          }
+        }
+#pragma unroll
+        for (int w = 0; w < kGroups; ++w) {              // sums of groups, moved to the lanes of their columns
+          part[w] += __shfl_xor_sync(0xffffffffu, part[w], 1);
+          part[w] += __shfl_xor_sync(0xffffffffu, part[w], 2);
+          qsum[w][n][0] = __shfl_sync(0xffffffffu, part[w], 8 * t);
+          qsum[w][n][1] = __shfl_sync(0xffffffffu, part[w], 8 * t + 4);
+        }
+      } else if (write) {
+#pragma unroll 4
+        for (int k = 0; k < D / 8; ++k) {                // steps 2 c, 2 c + 1: dimensions 16 c + 4 t + (0, 1) and (2, 3)
+          const int dim = 16 * (k / 2) + 4 * t + 2 * (k % 2);
+          const float x = at(dim), y = at(dim + 1), xh = tf32_high(x), yh = tf32_high(y);
+          shared[(k * NT + n) * 32 + lane] =
+              make_uint4(__float_as_uint(xh), __float_as_uint(yh), __float_as_uint(x - xh), __float_as_uint(y - yh));
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int c = 8 * n + 2 * t + e;
+        lim[n][e] = c < rows ? sg.len - a.nq + 1 + (sg.block * kRows + c) / G : 0;
+      }
+    }
+  }
+
+  __device__ __forceinline__ void logits(uint32_t at, const uint4* shared, float (&s)[NT][4], int lane) {
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+    if constexpr (MODE == kBf16) {
+      const int r = lane & 15;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        uint32_t x[4];
+        ldmatrix4(x, at + r * (2 * D) + 16 * ((2 * k + (lane >> 4)) ^ swizzle(r)));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma_bf16(s[n], x, q[k][n][0], q[k][n][1]);
+      }
+    } else if constexpr (MODE == kQ4) {
+      uint32_t x[kGroups], y[kGroups], px[kGroups], py[kGroups];   // tokens g and g + 8
+      if constexpr (D == 128) {
+        lds_words(x, at + g * 64 + 16 * (t ^ ((g >> 1) & 3)));
+        lds_words(y, at + (g + 8) * 64 + 16 * (t ^ ((g >> 1) & 3)));
+      } else {
+        lds_words(x, at + g * 32 + (8 * t ^ (16 * ((g >> 2) & 1))));
+        lds_words(y, at + (g + 8) * 32 + (8 * t ^ (16 * ((g >> 2) & 1))));
+      }
+      lds_words(px, at + kKPairs + g * (D / 8));
+      lds_words(py, at + kKPairs + (g + 8) * (D / 8));
+#pragma unroll
+      for (int w = 0; w < kGroups; ++w) {
+        float c[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) c[n][e] = 0.f;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t f[4] = {codes_at(x[w], 2 * k), codes_at(y[w], 2 * k), codes_at(x[w], 2 * k + 1), codes_at(y[w], 2 * k + 1)};
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            if constexpr (PARTS == 1) {
+              mma_bf16(c[n], f, q[2 * w + k][n][0], q[2 * w + k][n][1]);
+            } else {
+              const uint2* from = reinterpret_cast<const uint2*>(shared) + ((2 * w + k) * NT + n) * 3 * 32 + lane;
+#pragma unroll
+              for (int i = 2; i >= 0; --i) mma_bf16(c[n], f, from[32 * i].x, from[32 * i].y);
+            }
+          }
+        }
+        const float sx = high_f(px[w]), sy = high_f(py[w]);
+        const float lx = fmaf(-128.f, sx, low_f(px[w])), ly = fmaf(-128.f, sy, low_f(py[w]));
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            s[n][e] = fmaf(sx, c[n][e], fmaf(lx, qsum[w][n][e], s[n][e]));
+            s[n][2 + e] = fmaf(sy, c[n][2 + e], fmaf(ly, qsum[w][n][e], s[n][2 + e]));
+          }
+      }
+    } else {
+#pragma unroll 4
+      for (int c = 0; c < D / 16; ++c) {
+        const uint4 u = lds128(at + g * (4 * D) + 16 * ((4 * c + t) ^ swizzle(g)));
+        const uint4 v = lds128(at + (g + 8) * (4 * D) + 16 * ((4 * c + t) ^ swizzle(g)));
+        const uint32_t xs[4] = {u.x, u.y, u.z, u.w}, ys[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          uint32_t hi[4] = {xs[2 * k], ys[2 * k], xs[2 * k + 1], ys[2 * k + 1]}, lo[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float x = __uint_as_float(hi[i]), h = tf32_high(x);
+            hi[i] = __float_as_uint(h);
+            lo[i] = __float_as_uint(x - h);
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const uint4 f = shared[((2 * c + k) * NT + n) * 32 + lane];
+            mma_tf32(s[n], lo, f.x, f.y);
+            mma_tf32(s[n], hi, f.z, f.w);
+            mma_tf32(s[n], hi, f.x, f.y);
+          }
+        }
+      }
+    }
+  }
+
+  // O^T += V^T P^T for one unit.  p: weights in the layout of the logits.
+  // skip: tokens from `seen` on do not exist for this product (raw rows: their values are made zero).
+  __device__ __forceinline__ void values(uint32_t at, const float (&p)[NT][4], int seen, bool skip, int lane) {
+    const int g = lane >> 2, t = lane & 3;
+    if constexpr (MODE == kBf16) {
+      uint32_t b[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        b[n][0] = transpose8(pack_bf16(p[n][0], p[n][1]));
+        b[n][1] = transpose8(pack_bf16(p[n][2], p[n][3]));
+      }
+      const int r = (lane & 7) + 8 * (lane >> 4), c = (lane >> 3) & 1;
+      const uint32_t keep[2] = {(2 * t < seen ? 0xffffu : 0u) | (2 * t + 1 < seen ? 0xffff0000u : 0u),
+                                (2 * t + 8 < seen ? 0xffffu : 0u) | (2 * t + 9 < seen ? 0xffff0000u : 0u)};
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        uint32_t v[4];
+        ldmatrix4_trans(v, at + kV + r * (2 * D) + 16 * ((2 * i + c) ^ swizzle(r)));
+        if (skip) { v[0] &= keep[0]; v[1] &= keep[0]; v[2] &= keep[1]; v[3] &= keep[1]; }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma_bf16(O[i][n], v, b[n][0], b[n][1]);
+      }
+    } else if constexpr (MODE == kQ4) {
+      uint32_t px[kGroups], py[kGroups], cw[4][kGroups];
+      lds_words(px, at + kVPairs + g * (D / 8));
+      lds_words(py, at + kVPairs + (g + 8) * (D / 8));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {                      // tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+        const int r = 2 * t + (j & 1) + 8 * (j >> 1);
+        if constexpr (D == 128) lds_words(cw[j], at + kV + r * 64 + 16 * ((g >> 1) ^ ((r >> 1) & 3)));
+        else lds_words(cw[j], at + kV + r * 32 + (8 * (g >> 1) ^ (16 * ((r >> 2) & 1))));
+      }
+      const uint32_t half = (g & 1) ? 0x7632u : 0x5410u; // upper or lower halves of two words
+      constexpr uint32_t minus[4] = {0xc300c300u, 0xc300c300u, 0xc300c300u, 0xc300c300u};
+#pragma unroll
+      for (int w = 0; w < kGroups; ++w) {
+        const float sx = high_f(px[w]), sy = high_f(py[w]), lx = low_f(px[w]), ly = low_f(py[w]);
+        uint32_t b[NT][PARTS][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            x[e] = p[n][e] * sx;
+            x[2 + e] = p[n][2 + e] * sy;
+            float a = p[n][e] * lx, c = p[n][2 + e] * ly;
+            if (skip) {                                  // (a token that is not seen may have any step and lo)
+              if (p[n][e] == 0.f) { x[e] = 0.f; a = 0.f; }
+              if (p[n][2 + e] == 0.f) { x[2 + e] = 0.f; c = 0.f; }
+            }
+            off[n][e][w] += a + c;
+          }
+          if constexpr (PARTS == 1) {
+            b[n][0][0] = transpose8(pack_bf16(x[0], x[1]));
+            b[n][0][1] = transpose8(pack_bf16(x[2], x[3]));
+          } else {
+            uint32_t u[3], v[3];
+            three_parts(x[0], x[1], u);
+            three_parts(x[2], x[3], v);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) { b[n][i][0] = transpose8(u[i]); b[n][i][1] = transpose8(v[i]); }
+          }
+        }
+        const uint32_t u = __byte_perm(cw[0][w], cw[1][w], half), v = __byte_perm(cw[2][w], cw[3][w], half);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t f[4] = {codes_at(u, 2 * j), codes_at(u, 2 * j + 1), codes_at(v, 2 * j), codes_at(v, 2 * j + 1)};
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = PARTS - 1; i >= 0; --i) {
+              mma_bf16(O[2 * w + j][n], f, b[n][i][0], b[n][i][1]);
+              mma_bf16(O[2 * w + j][n], minus, b[n][i][0], b[n][i][1]);
+            }
+        }
+      }
+    } else {
+      // weights as B fragments: lane (g, t) needs row g's weights of tokens t + 4 j, which lanes 4 (t + 4 j) + g / 2 hold
+      uint32_t hi[NT][4], lo[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int from = 4 * (t + 4 * (j & 1)) + (g >> 1);
+          const float x = __shfl_sync(0xffffffffu, p[n][2 * (j >> 1)], from), y = __shfl_sync(0xffffffffu, p[n][2 * (j >> 1) + 1], from);
+          const float w = (g & 1) ? y : x, h = tf32_high(w);
+          hi[n][j] = __float_as_uint(h);
+          lo[n][j] = __float_as_uint(w - h);
+        }
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t v[4][4];                                // tokens t + 4 j, dimensions 32 c + 4 g ..
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int r = t + 4 * j;
+          const uint4 u = lds128(at + kV + r * (4 * D) + 16 * ((8 * c + g) ^ swizzle(r)));
+          const bool keep = !skip || r < seen;
+          v[j][0] = keep ? u.x : 0u; v[j][1] = keep ? u.y : 0u; v[j][2] = keep ? u.z : 0u; v[j][3] = keep ? u.w : 0u;
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)                      // tokens 8 k ..
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            uint32_t h[4] = {v[2 * k][2 * i], v[2 * k][2 * i + 1], v[2 * k + 1][2 * i], v[2 * k + 1][2 * i + 1]}, x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float f = __uint_as_float(h[e]), fh = tf32_high(f);
+              h[e] = __float_as_uint(fh);
+              x[e] = isfinite(f) ? __float_as_uint(f - fh) : 0u;
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              mma_tf32(O[2 * c + i][n], x, hi[n][2 * k], hi[n][2 * k + 1]);
+              mma_tf32(O[2 * c + i][n], h, lo[n][2 * k], lo[n][2 * k + 1]);
+              mma_tf32(O[2 * c + i][n], h, hi[n][2 * k], hi[n][2 * k + 1]);
+            }
+          }
+      }
+    }
+  }
+
+  // One unit: tokens from `token` on, the first `rows` of them in shared memory at `at`.
+  __device__ __forceinline__ void unit(uint32_t at, const uint4* shared, int token, int rows, int len, int nq, float c, int lane) {
+    const int g = lane >> 2;
+    float s[NT][4];
+    logits(at, shared, s, lane);
+    const bool edge = rows < kUnit || token + kUnit > len - nq + 1;
+    if (edge) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = g + 8 * (e >> 1);
+          if (r >= rows || token + r >= lim[n][e & 1]) s[n][e] = -INFINITY;
+        }
+    }
+    bool raise = false;
+    float top[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        top[n][e] = fmaxf(s[n][e], s[n][2 + e]);
+        raise |= (top[n][e] - m[n][e]) * c > kRaise || (m[n][e] == -INFINITY && top[n][e] > -INFINITY);
+      }
+    if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float x = top[n][e];
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+          x = fmaxf(x, m[n][e]);
+          const float f = x == -INFINITY ? 1.f : ex2((m[n][e] - x) * c);
+          m[n][e] = x;
+          l[n][e] *= f;
+#pragma unroll
+          for (int w = 0; w < (MODE == kQ4 ? kGroups : 1); ++w) off[n][e][w] *= f;
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) { O[i][n][e] *= f; O[i][n][2 + e] *= f; }
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float use = m[n][e] == -INFINITY ? 0.f : m[n][e] * c;
+        s[n][e] = ex2(fmaf(s[n][e], c, -use));
+        s[n][2 + e] = ex2(fmaf(s[n][2 + e], c, -use));
+        l[n][e] += s[n][e] + s[n][2 + e];
+      }
+    if (MODE == kQ4 || nq == 1 || !edge) {
+      values(at, s, kUnit, MODE == kQ4 && edge, lane);
+      return;
+    }
+    // Some queries see fewer of these tokens than others: one product per distinct number, from values that are zero
+    // beyond it, and of each only the columns that it is for (a weight of zero times an infinity would be NaN).
+    int done = -1;
+    while (true) {
+      int next = kUnit + 1;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int v = min(max(lim[n][e] - token, 0), rows);
+          if (v > done) next = min(next, v);
+        }
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) next = min(next, __shfl_xor_sync(0xffffffffu, next, o));
+      if (next > kUnit) break;
+      done = next;
+      if (next == 0) continue;
+      float keep[D / 16][NT][4];
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) keep[i][n][e] = O[i][n][e];
+      values(at, s, next, true, lane);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (min(max(lim[n][e & 1] - token, 0), rows) != next) {
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) O[i][n][e] = keep[i][n][e];
+          }
+    }
+  }
+
+  // Dimension of element e of O[i] in this lane.
+  static __device__ __forceinline__ int dim_of(int i, int e, int g) {
+    if constexpr (MODE == kBf16) return 16 * i + g + 8 * (e >> 1);
+    return 32 * (i >> 1) + 4 * g + 2 * (i & 1) + (e >> 1);
+  }
+};
+
+template <typename T, int MODE, int D, int NT>
+__global__ void __launch_bounds__(kThreads, ctas_per_sm<MODE, D, NT>()) cached_kernel(const CachedArgs a, int least) {
+  constexpr int PARTS = sizeof(T) == 4 && MODE == kQ4 ? 3 : 1, S = stages<MODE, D>();
+  using W = Warp<MODE, D, NT, PARTS>;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ Walk walk;
+  __shared__ float ms[kWarps][8 * NT], ls[kWarps][8 * NT];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  uint4* queries = reinterpret_cast<uint4*>(smem + (size_t)kWarps * S * W::kUnitBytes);
+  const uint32_t ring = tc::smem_u32(smem) + warp * S * W::kUnitBytes;
+  const float c = a.scale * kLog2e;
+  const int G = a.H / a.Hk;
+  W w;
+  Segment sg;
+  for (bool more = walk_begin(a, least, walk, sg); more; more = walk_next(a, walk, sg)) {
+    const int first = sg.unit + warp, end = sg.unit + sg.n;
+    const int mine = first < end ? (end - first + kWarps - 1) / kWarps : 0;
+    const int32_t* table = a.table + (int64_t)sg.b * a.table_pages;
+    auto page_at = [&](int k) {                            // physical page of this warp's k-th unit
+      return k < mine ? table[(first + k * kWarps) * kUnit / a.page] : 0;
+    };
+    auto fetch = [&](int k, int page) {
+      if (k < mine) {
+        const int token = (first + k * kWarps) * kUnit;
+        const bool ok = page >= 0 && page < a.pages;
+        if (!ok && lane == 0) report(a.status, DEV_BAD_INDEX);
+        W::fetch(ring + (k % S) * W::kUnitBytes, a, ok ? page : -1, sg.hk, token % a.page, min(kUnit, sg.len - token), lane);
+      }
+      cp_async_commit();
+    };
+    int ahead = 0;
+#pragma unroll
+    for (int k = 0; k < S - 1; ++k) fetch(k, page_at(k));
+    ahead = page_at(S - 1);
+    w.clear();
+    if (MODE == kF32 || PARTS == 3) __syncthreads();       // (the segment before is done with the shared queries)
+    w.template load_queries<T>(a, sg, queries, warp == 0, lane);
+    if (MODE == kF32 || PARTS == 3) __syncthreads();
+    for (int k = 0; k < mine; ++k) {
+      cp_async_wait<S - 2>();
+      __syncwarp();
+      const int token = (first + k * kWarps) * kUnit;
+      const int page = page_at(k);
+      const int rows = page >= 0 && page < a.pages ? min(kUnit, sg.len - token) : 0;
+      fetch(k + S - 1, ahead);
+      ahead = page_at(k + S);
+      w.unit(ring + (k % S) * W::kUnitBytes, queries, token, rows, sg.len, a.nq, c, lane);
+      __syncwarp();
+    }
+    cp_async_wait<0>();
+    // ---- the warps' results added: maxima, sums and outputs through shared memory, in the order of the warps
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+          w.l[n][e] += __shfl_xor_sync(0xffffffffu, w.l[n][e], o);
+#pragma unroll
+          for (int x = 0; x < (MODE == kQ4 ? W::kGroups : 1); ++x)
+            if (MODE == kQ4) w.off[n][e][x] += __shfl_xor_sync(0xffffffffu, w.off[n][e][x], o);
+        }
+        if (g == 0) { ms[warp][8 * n + 2 * t + e] = w.m[n][e]; ls[warp][8 * n + 2 * t + e] = w.l[n][e]; }
+      }
+    __syncthreads();                                       // (every warp is done with its ring: it holds the outputs now)
+    float* out = reinterpret_cast<float*>(smem);           // [kWarps][8 NT][D + 4]
+    constexpr int kPitch = D + 4;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = 8 * n + 2 * t + e;
+        float top = ms[0][r];
+#pragma unroll
+        for (int x = 1; x < kWarps; ++x) top = fmaxf(top, ms[x][r]);
+        const float f = w.m[n][e] == -INFINITY ? 0.f : ex2((w.m[n][e] - top) * c);
+        float* row = out + (warp * 8 * NT + r) * kPitch;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float v = w.O[i][n][2 * h + e];
+            if constexpr (MODE == kQ4) v += w.off[n][e][i >> 1];
+            row[W::dim_of(i, 2 * h, g)] = f == 0.f ? 0.f : v * f;
+          }
+      }
+    __syncthreads();
+    const int rows = min(kRows, a.nq * G - sg.block * kRows);
+    float* slot = segment_slot(a, sg);
+    for (int r = warp; r < rows; r += kWarps) {
+      float top = ms[0][r], sum = 0.f;
+#pragma unroll
+      for (int x = 1; x < kWarps; ++x) top = fmaxf(top, ms[x][r]);
+#pragma unroll
+      for (int x = 0; x < kWarps; ++x) sum += ms[x][r] == -INFINITY ? 0.f : ls[x][r] * ex2((ms[x][r] - top) * c);
+      const int q = sg.block * kRows + r;
+      const int64_t token = (int64_t)sg.b * a.nq + q / G;
+      const int h = sg.hk * G + q % G;
+      constexpr int kPer = D / 32;
+      float y[kPer] = {};
+#pragma unroll
+      for (int x = 0; x < kWarps; ++x)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) y[i] += out[(x * 8 * NT + r) * kPitch + kPer * lane + i];
+      if (slot) {
+        if (lane == 0) { slot[r] = top == -INFINITY ? -INFINITY : top * c; slot[kRows + r] = sum; }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) slot[2 * kRows + r * D + kPer * lane + i] = y[i];
+      } else {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        T* Y = static_cast<T*>(a.Y) + token * a.y_stride + (int64_t)h * D + kPer * lane;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) Y[i] = from_f32<T>(y[i] * inv);
+        if (a.lse && lane == 0) a.lse[token * a.H + h] = sum == 0.f ? -INFINITY : (top * c + log2f(sum)) * kLn2;
+      }
+    }
+    __syncthreads();                                       // (the ring may be filled again)
+  }
+}
+
+template <typename T, int MODE, int D, int NT>
+avq_status launch(const CachedArgs& a, int dtype, cudaStream_t st) {
+  constexpr int PARTS = sizeof(T) == 4 && MODE == kQ4 ? 3 : 1;
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return AVQ_ERR_CUDA;
+  avq_status s = open_shared_memory<cached_kernel<T, MODE, D, NT>>(dev);
+  if (s != AVQ_OK) return s;
+  const int ctas = min(sms * ctas_per_sm<MODE, D, NT>(), kMaxCtas), least = 2 * kWarps;
+  cached_kernel<T, MODE, D, NT><<<ctas, kThreads, cached_smem<MODE, D, NT, PARTS>(), st>>>(a, least);
+  s = cuda_ok(cudaGetLastError());
+  return s == AVQ_OK ? join(a, dtype, ctas, least, st) : s;
+}
+template <typename T, int MODE>
+avq_status launch_rows(const CachedArgs& a, int dtype, cudaStream_t st) {
+  const bool few = a.nq * (a.H / a.Hk) <= 8;
+  if (a.d == 64) return few ? launch<T, MODE, 64, 1>(a, dtype, st) : launch<T, MODE, 64, 2>(a, dtype, st);
+  return few ? launch<T, MODE, 128, 1>(a, dtype, st) : launch<T, MODE, 128, 2>(a, dtype, st);
+}
+
+}  // namespace
+
+avq_status tc_cached(const CachedArgs& a, int dtype, int bits, cudaStream_t st) {
+  if (dtype == AVQ_F32) return bits == 4 ? launch_rows<float, kQ4>(a, dtype, st) : launch_rows<float, kF32>(a, dtype, st);
+  return bits == 4 ? launch_rows<__nv_bfloat16, kQ4>(a, dtype, st) : launch_rows<__nv_bfloat16, kBf16>(a, dtype, st);
+}
+
+}  // namespace exact
+}  // namespace avq
