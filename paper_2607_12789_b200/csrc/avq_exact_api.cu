@@ -1,5 +1,5 @@
 // C ABI of the exact operators: argument validation and dispatch.  The kernels live in avq_exact_simt.cu (CUDA cores,
-// and the joining of split sequences), avq_tc_cached.cu (tensor cores) and avq_cache.cu (rows into and out of a cache).
+// and the joining of split sequences), avq_tc_prompt.cu and avq_tc_cached.cu (tensor cores) and avq_cache.cu (rows into and out of a cache).
 #include "avq_exact.cuh"
 
 namespace avq {
@@ -96,7 +96,7 @@ avq_status avq_prompt_attend(const avq_heads* heads, const void* Q, int64_t q_st
   const PromptArgs a = {Q, K, V, Y, lse_out, cu_q, cu_k, q_stride, k_stride, v_stride, y_stride, h.H, h.Hk, h.d, S, Tq, Tk,
                         (h.flags & AVQ_FLAG_CAUSAL) ? 1 : 0, h.scale, static_cast<int32_t*>(workspace)};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return simt_prompt(a, h.dtype, st);
+  return h.dtype == AVQ_BF16 && tensor_path(h) ? tc_prompt(a, st) : simt_prompt(a, h.dtype, st);
 }
 
 size_t avq_cache_bytes(const avq_cache* cache) {

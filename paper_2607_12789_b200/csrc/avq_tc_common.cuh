@@ -454,6 +454,8 @@ EncodeTiledFn encode_tiled_fn();   // nullptr if the driver entry point cannot b
 // and 128-byte swizzle; out-of-range elements read as zero.
 avq_status make_tmap_bf16(CUtensorMap* map, const void* base, int rank, const uint64_t* dims,
                           const uint32_t* box);
+// bf16 rows of several heads: dims[0] = d, dims[1] = heads (dense), dims[2] = rows, `stride` elements apart; boxes as above.
+avq_status make_tmap_rows(CUtensorMap* map, const void* base, const uint64_t (&dims)[3], int64_t stride, const uint32_t (&box)[3]);
 // Codeword rows [rows, d] bf16 in boxes of `box_rows` rows x 64 columns that land in shared memory with row 4 v + t of
 // every group of 8 at position 2 t + v: a 4-dimensional view (column, v, t, group).
 avq_status make_tmap_codes(CUtensorMap* map, const void* base, int d, uint64_t rows, uint32_t box_rows);

@@ -95,6 +95,16 @@ avq_status make_tmap_bf16(CUtensorMap* map, const void* base, int rank, const ui
   return encode(map, key);
 }
 
+avq_status make_tmap_rows(CUtensorMap* map, const void* base, const uint64_t (&dims)[3], int64_t stride, const uint32_t (&box)[3]) {
+  TmapKey key = {};
+  key.base = base;
+  key.rank = 3;
+  for (int i = 0; i < 3; ++i) { key.dims[i] = dims[i]; key.box[i] = box[i]; }
+  key.strides[0] = 2 * dims[0];
+  key.strides[1] = 2 * (uint64_t)stride;
+  return encode(map, key);
+}
+
 avq_status make_tmap_codes(CUtensorMap* map, const void* base, int d, uint64_t rows, uint32_t box_rows) {
   if (rows % 8 != 0 || box_rows % 8 != 0) return AVQ_ERR_UNSUPPORTED;
   const uint64_t row = 2 * (uint64_t)d;
