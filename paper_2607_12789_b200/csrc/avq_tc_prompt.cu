@@ -28,6 +28,7 @@ using namespace tc;
 constexpr int kTile = 128, kThreads = 384, kLoader = 8, kIssuer = 9, kGuards = 64;
 constexpr int kReady = 8;                                  // value tiles that the guards can be ahead by, at least
 constexpr float kRaise = 8.f;
+constexpr int kFewRegs = 80, kManyRegs = 208;              // per thread of warps 8-11, of warps 0-7
 template <int D> __host__ __device__ constexpr int ring_slots() { return D == 128 ? 5 : 10; }
 template <int D> __host__ __device__ constexpr int tile_bytes() { return kTile * D * 2; }
 template <int D> __host__ __device__ constexpr size_t prompt_smem() { return 1024 + (size_t)(2 + ring_slots<D>()) * tile_bytes<D>(); }
@@ -186,6 +187,10 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   auto turn_of = [&](int e) { return (e & 1) && (e >> 1) >= guarded ? ((e >> 1) - guarded) / kReady : e / kSlots; };
   auto landing = [&](int e) { return (e & 1) && (e >> 1) >= guarded ? &sh.raw[((e >> 1) - guarded) % kReady] : &sh.full[e % kSlots]; };
 
+  // The softmax needs the registers: a row of logits is 128 of them.  (What the block was launched with covers the shares:
+  // the host checks it.)  Each warp of a group of four moves its share in its own branch.
+  if (warp >= kLoader) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
   if (warp == kLoader) {
     int e = 0;
     bool ok = true;
@@ -308,7 +313,9 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       fence_proxy_async();
       mbar_arrive(&sh.cleaned[(j - guarded) % kReady]);
     }
+  }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegs));
     const int i = warp >> 2, r = threadIdx.x & 127;
     const Rows rows = i ? row1 : row0;
     const uint32_t at = tmem + ((uint32_t)(32 * (warp & 3)) << 16), at_s = at + 128 * i, at_o = at + kColO + 128 * i;
@@ -441,6 +448,17 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   if (warp == kIssuer) tmem_dealloc(tmem, 512);
 }
 
+// Whether the block's registers at launch cover the shares that its warps ask for (or they would wait for good).
+template <int D>
+bool registers_cover() {
+  static const bool ok = [] {
+    cudaFuncAttributes fa;
+    return cudaFuncGetAttributes(&fa, prompt_tc_kernel<D>) == cudaSuccess &&
+           fa.numRegs * kThreads >= 32 * (kLoader * kManyRegs + (kThreads / 32 - kLoader) * kFewRegs);
+  }();
+  return ok;
+}
+
 template <int D>
 avq_status launch(const PromptArgs& a, cudaStream_t st) {
   const int G = a.H / a.Hk, per = kTile / G;
@@ -458,6 +476,7 @@ avq_status launch(const PromptArgs& a, cudaStream_t st) {
   if (cudaGetDevice(&dev) != cudaSuccess) return AVQ_ERR_CUDA;
   s = open_shared_memory<prompt_tc_kernel<D>>(dev);
   if (s != AVQ_OK) return s;
+  if (!registers_cover<D>()) return AVQ_ERR_CUDA;
   const int64_t grid = most_pieces(a.Tq, a.S, 2 * per) * a.Hk;
   if (grid >= (int64_t)1 << 31) return AVQ_ERR_UNSUPPORTED;
   prompt_tc_kernel<D><<<(unsigned)grid, kThreads, prompt_smem<D>(), st>>>(tmQ, tmK, tmV, a);
