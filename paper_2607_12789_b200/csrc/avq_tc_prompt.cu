@@ -26,6 +26,7 @@ namespace {
 using namespace tc;
 
 constexpr int kTile = 128, kThreads = 384, kLoader = 8, kIssuer = 9, kGuards = 64;
+constexpr int kMost = 96;                                  // weights of a tile that the product starts with
 constexpr int kReady = 8;                                  // value tiles that the guards can be ahead by, at least
 constexpr float kRaise = 8.f;
 constexpr int kFewRegs = 80, kManyRegs = 208;              // per thread of warps 8-11, of warps 0-7
@@ -34,7 +35,7 @@ template <int D> __host__ __device__ constexpr int tile_bytes() { return kTile *
 template <int D> __host__ __device__ constexpr size_t prompt_smem() { return 1024 + (size_t)(2 + ring_slots<D>()) * tile_bytes<D>(); }
 
 struct Shared {
-  uint64_t q_full, full[10], empty[10], raw[kReady], cleaned[kReady], s_full[2], p_ready[2], done[2], drained;
+  uint64_t q_full, full[10], empty[10], raw[kReady], cleaned[kReady], s_full[2], p_most[2], p_ready[2], done[2], drained;
   Piece piece;
   uint32_t tmem;
   int found, abort_flag, wide;
@@ -112,6 +113,53 @@ __device__ __forceinline__ void poly_ex2(f32x2 x, float& lo, float& hi) {
 }
 constexpr int kPolyOf8 = 2;                                // pairs of 8 whose exponentials the polynomial computes
 
+// What is added to scale * logit, in powers of two: an infinite or NaN maximum makes every weight of the row NaN.
+__device__ __forceinline__ float reference(float m, float c) {
+  return m == -INFINITY ? 0.f : isfinite(m) ? -m * c : __int_as_float(0x7fffffff);
+}
+__device__ __forceinline__ float row_max(const uint32_t (&s)[4][32]) {
+  float top[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    top[q] = max3_nan(__uint_as_float(s[q][0]), __uint_as_float(s[q][1]), __uint_as_float(s[q][31]));
+#pragma unroll
+    for (int k = 2; k + 1 < 31; k += 2) top[q] = max3_nan(top[q], __uint_as_float(s[q][k]), __uint_as_float(s[q][k + 1]));
+    top[q] = max3_nan(top[q], __uint_as_float(s[q][30]), __uint_as_float(s[q][30]));
+  }
+  return max3_nan(max3_nan(top[0], top[1], top[2]), top[3], top[3]);
+}
+// Weights of the 32-column quarters FROM .. TO - 1 of a row, as bfloat16 over the row's logits in tensor memory; returns
+// their sum.  EDGE: the tile holds masked logits, whose weights have to be exactly zero (no polynomial).  mx: gets the
+// maximum of the whole row.
+template <bool EDGE, int FROM, int TO>
+__device__ __forceinline__ float weights(const uint32_t (&s)[4][32], float c, float sub, uint32_t at, float* mx) {
+  const f32x2 c2 = pack2(c, c), sub2 = pack2(sub, sub);
+  f32x2 sum[2] = {0ull, 0ull};
+  if (mx) *mx = row_max(s);
+#pragma unroll
+  for (int q = FROM; q < TO; ++q) {
+    uint32_t p[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const f32x2 x = fma2(pack2u(s[q][2 * k], s[q][2 * k + 1]), c2, sub2);
+      float lo, hi;
+      if (!EDGE && (k & 7) >= 8 - kPolyOf8) {
+        poly_ex2(x, lo, hi);
+      } else {
+        unpack2(x, lo, hi);
+        lo = ex2(lo);
+        hi = ex2(hi);
+      }
+      sum[k & 1] = add2(sum[k & 1], pack2(lo, hi));
+      p[k] = pack_bf16(lo, hi);
+    }
+    tmem_st16(at + 16 * q, p);
+  }
+  float lo, hi;
+  unpack2(add2(sum[0], sum[1]), lo, hi);
+  return lo + hi;
+}
+
 // What of a tile of rows a CTA needs to know.
 struct Rows {
   int count;       // tokens of the tile that exist
@@ -152,7 +200,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     mbar_init(&sh.q_full, 1);
     for (int i = 0; i < kSlots; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
     for (int i = 0; i < kReady; ++i) { mbar_init(&sh.raw[i], 1); mbar_init(&sh.cleaned[i], kGuards); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_ready[i], kTile); mbar_init(&sh.done[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_most[i], kTile); mbar_init(&sh.p_ready[i], kTile); mbar_init(&sh.done[i], 1); }
     mbar_init(&sh.drained, 1);
     sh.abort_flag = 0;
     sh.wide = 0;
@@ -230,9 +278,9 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       }
       umma_commit(&sh.s_full[i]);
     };
-    auto issue_o = [&](int i, int slot, bool more) {
+    auto issue_o = [&](int i, int slot, int from, int to, bool more) {
 #pragma unroll
-      for (int k = 0; k < kTile / 16; ++k)
+      for (int k = from; k < to; ++k)
         umma_bf16_ts(tmem + kColO + 128 * i, tmem + 128 * i + 8 * k,
                      umma_desc_sw128_mn(r_at + slot * tile_bytes<D>() + k * 2048, kSubBytes), kIdO, more || k > 0);
     };
@@ -255,11 +303,15 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       for (int i = 0; i < 2; ++i) {
         const int n = i ? row1.tiles : row0.tiles;
         if (j < n) {
-          ok = ok && wait_warp(&sh.p_ready[i], j & 1);
+          ok = ok && wait_warp(&sh.p_most[i], j & 1);
           if (!ok) break;
           tc_fence_after();
+          if (elect_one()) issue_o(i, ev % kSlots, 0, kMost / 16, j > 0);
+          __syncwarp();
+          if (!(ok = wait_warp(&sh.p_ready[i], j & 1))) break;
+          tc_fence_after();
           if (elect_one()) {
-            issue_o(i, ev % kSlots, j > 0);
+            issue_o(i, ev % kSlots, kMost / 16, kTile / 16, true);
             if (j + 1 < n) issue_s(i, ek % kSlots);
             else umma_commit(&sh.done[i]);
           }
@@ -341,16 +393,11 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           for (int k = 0; k < 32; ++k)
             if (32 * q + k >= n) s[q][k] = 0xff800000u;
       }
-      float top[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        top[q] = max3_nan(__uint_as_float(s[q][0]), __uint_as_float(s[q][1]), __uint_as_float(s[q][2]));
-#pragma unroll
-        for (int k = 3; k + 1 < 32; k += 2) top[q] = max3_nan(top[q], __uint_as_float(s[q][k]), __uint_as_float(s[q][k + 1]));
-        top[q] = max3_nan(top[q], __uint_as_float(s[q][31]), __uint_as_float(s[q][31]));
-      }
-      const float mx = max3_nan(max3_nan(top[0], top[1], top[2]), top[3], top[3]);
-      // (of the first tile, and where there is a NaN, the difference is no number)
+      // The weights of all but the last quarter are taken with the maximum of the tiles before; the tile's own is found on
+      // the side.  Only where it is higher by 2^8 (or there is none before, or a NaN) they are taken again.
+      float mx = -INFINITY, sum = 0.f;
+      if (j == 0) mx = row_max(s);
+      else sum = edge ? weights<true, 0, kMost / 32>(s, c, reference(m, c), at_s, &mx) : weights<false, 0, kMost / 32>(s, c, reference(m, c), at_s, &mx);
       if (__any_sync(0xffffffffu, !((mx - m) * c <= kRaise))) {
         const float up = max3_nan(m, mx, mx);
         const float f = up == m || up == -INFINITY ? 1.f : ex2((m - up) * c);
@@ -368,36 +415,16 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             tmem_st32(at_o + 32 * q, o);
           }
         }
-      }
-      // an infinite or NaN maximum makes every weight of the row NaN
-      const float sub = m == -INFINITY ? 0.f : isfinite(m) ? -m * c : __int_as_float(0x7fffffff);
-      const f32x2 c2 = pack2(c, c), sub2 = pack2(sub, sub);
-      f32x2 sum[2] = {0ull, 0ull};
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint32_t p[16];
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const f32x2 x = fma2(pack2u(s[q][2 * k], s[q][2 * k + 1]), c2, sub2);
-          float lo, hi;
-          if ((k & 7) >= 8 - kPolyOf8 && !edge) {
-            poly_ex2(x, lo, hi);
-          } else {
-            unpack2(x, lo, hi);
-            lo = ex2(lo);
-            hi = ex2(hi);
-          }
-          sum[k & 1] = add2(sum[k & 1], pack2(lo, hi));
-          p[k] = pack_bf16(lo, hi);
-        }
-        tmem_st16(at_s + 16 * q, p);
+        sum = weights<true, 0, kMost / 32>(s, c, reference(m, c), at_s, nullptr);
       }
       tmem_st_wait();
       tc_fence_before();
+      mbar_arrive(&sh.p_most[i]);
+      sum += edge ? weights<true, kMost / 32, 4>(s, c, reference(m, c), at_s, nullptr) : weights<false, kMost / 32, 4>(s, c, reference(m, c), at_s, nullptr);
+      tmem_st_wait();
+      tc_fence_before();
       mbar_arrive(&sh.p_ready[i]);
-      float lo, hi;
-      unpack2(add2(sum[0], sum[1]), lo, hi);
-      l += lo + hi;
+      l += sum;
     }
     if (ok && rows.tiles > 0) ok = wait_warp(&sh.done[i], 0);
     if (ok && rows.tiles > guarded && rows.tiles > 0) {    // (whether a value was set to zero)
