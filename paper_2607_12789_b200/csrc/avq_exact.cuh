@@ -45,8 +45,8 @@ struct AppendArgs {
   const int32_t* slots;
   const float *cos, *sin;
   const int32_t* pos;
-  int64_t k_stride, v_stride, q_stride, q_out_stride, rows;   // rows: T * (H + 2 Hk)
-  int32_t H, Hk, d, page, pages, angles, rot, adjacent;
+  int64_t k_stride, v_stride, q_stride, q_out_stride;
+  int32_t T, H, Hk, d, page, pages, angles, rot, adjacent;
   int32_t* status;
 };
 
@@ -54,8 +54,8 @@ struct ReadArgs {
   const void *keys, *values;
   void *K, *V;
   const int32_t* slots;
-  int64_t k_stride, v_stride, rows;                        // rows: T * 2 Hk
-  int32_t Hk, d, page, pages;
+  int64_t k_stride, v_stride;
+  int32_t T, Hk, d, page, pages;
   int32_t* status;
 };
 
@@ -109,8 +109,12 @@ __device__ __forceinline__ int q4_pair_at(int row, int d, int page, int group) {
 }
 __device__ __forceinline__ void q4_decode8(uint32_t word, uint32_t pair, float (&v)[8]) {
   const float lo = __uint_as_float(pair << 16), step = __uint_as_float(pair & 0xffff0000u);
+  // a code in the low bits of 2^23 is the float 2^23 + code (cheaper than a conversion)
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = __fadd_rn(lo, __fmul_rn((float)((word >> (4 * i)) & 15u), step));
+  for (int i = 0; i < 8; ++i) {
+    const float c = __fadd_rn(__uint_as_float(((word >> (4 * i)) & 15u) | 0x4b000000u), -8388608.f);
+    v[i] = __fadd_rn(lo, __fmul_rn(c, step));
+  }
 }
 
 // ---------------------------------------------------------------- packed batches

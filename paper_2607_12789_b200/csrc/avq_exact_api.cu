@@ -130,10 +130,10 @@ avq_status avq_cache_append(const avq_cache* cache, const void* K, int64_t k_str
   if (turn && (!rot->cos || !rot->sin || !rot->pos)) return AVQ_ERR_NULL;
   const int heads = (Q ? H : 0) + 2 * c.Hk;
   const AppendArgs a = {K, V, Q, c.keys, c.values, Q_out, slots, turn ? rot->cos : nullptr, turn ? rot->sin : nullptr,
-                        turn ? rot->pos : nullptr, k_stride, v_stride, q_stride, q_out_stride, (int64_t)T * heads,
+                        turn ? rot->pos : nullptr, k_stride, v_stride, q_stride, q_out_stride, T,
                         Q ? H : 0, c.Hk, c.d, c.page, c.pages, turn ? rot->rows : 0, turn ? rot->dims : 0,
                         turn ? rot->adjacent : 0, static_cast<int32_t*>(header)};
-  if (a.rows >= (int64_t)1 << 34) return AVQ_ERR_UNSUPPORTED;
+  if ((int64_t)T * heads >= (int64_t)1 << 34) return AVQ_ERR_UNSUPPORTED;
   return cache_append(a, c.dtype, c.bits, static_cast<cudaStream_t>(stream));
 }
 
@@ -148,9 +148,9 @@ avq_status avq_cache_read(const avq_cache* cache, const int32_t* slots, int32_t 
   AVQ_TRY(validate_rows(K, k_stride, c.Hk, c.d, c.dtype));
   AVQ_TRY(validate_rows(V, v_stride, c.Hk, c.d, c.dtype));
   AVQ_TRY(validate_header(header));
-  const ReadArgs a = {c.keys, c.values, K, V, slots, k_stride, v_stride, (int64_t)T * 2 * c.Hk, c.Hk, c.d, c.page, c.pages,
+  const ReadArgs a = {c.keys, c.values, K, V, slots, k_stride, v_stride, T, c.Hk, c.d, c.page, c.pages,
                       static_cast<int32_t*>(header)};
-  if (a.rows >= (int64_t)1 << 34) return AVQ_ERR_UNSUPPORTED;
+  if ((int64_t)T * 2 * c.Hk >= (int64_t)1 << 34) return AVQ_ERR_UNSUPPORTED;
   return cache_read(a, c.dtype, c.bits, static_cast<cudaStream_t>(stream));
 }
 
