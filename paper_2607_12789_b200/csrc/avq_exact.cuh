@@ -203,10 +203,6 @@ __device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* scratch) {
   for (int w = 0; w < (int)(blockDim.x >> 5); ++w) s += scratch[w];
   return s;
 }
-__device__ __forceinline__ int64_t run_of(int64_t total, int ctas, int least) {
-  const int64_t run = (total + ctas - 1) / ctas;
-  return run < least ? least : run;
-}
 
 // The physical page of a sequence's token, or -1 (reported) if the table holds no usable one.
 __device__ __forceinline__ int page_of(const CachedArgs& a, int b, int token) {
@@ -220,68 +216,89 @@ struct Segment {
   int32_t b, hk, block, len;
   int32_t unit, n, units;
 };
-struct Walk {                    // one thread's bookkeeping is every thread's: kept in shared memory
-  int64_t scratch[34];
-  int64_t at, end, before;       // first unit not yet handed out, end of the run, first unit of sequence b
+struct Place {                   // of the first unit not yet handed out
+  int64_t at, before;            // its number, the number of the first unit of sequence b
   int32_t b;
 };
-// Every thread of the block calls these two and gets the same segment; false: the run is over.
-__device__ __forceinline__ bool walk_next(const CachedArgs& a, Walk& w, Segment& sg) {
+struct Walk {                    // shared: every thread reads one place and the first writes the next beside it
+  int64_t scratch[34], end;      // end of the CTA's run
+  Place place[2];
+};
+// (64-bit divisions are long; nearly all are of numbers that fit 32 bits.)
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
+  return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+}
+__device__ __forceinline__ int64_t run_of(int64_t total, int ctas, int least) {
+  const int64_t run = quotient(total + ctas - 1, ctas);
+  return run < least ? least : run;
+}
+// Every thread of the block calls these two and gets the same segment; false: the run is over.  `turn`: 0, 1, ... of the
+// calls.  Between two calls the block meets at a barrier.
+__device__ __forceinline__ bool walk_next(const CachedArgs& a, Walk& w, Segment& sg, int turn) {
   const int per = segments_per_sequence(a), blocks = per / a.Hk;
-  __syncthreads();
-  int64_t at = w.at, before = w.before;
+  const Place p = w.place[turn & 1];
   const int64_t end = w.end;
-  int b = w.b;
-  __syncthreads();
-  if (at >= end) return false;
-  int len = clipped_len(a, b, false), U = units_of(len);
-  while (at >= before + (int64_t)U * per) {                // (ends: at < end <= all units)
+  if (p.at >= end) return false;
+  int64_t before = p.before;
+  int b = p.b, len = clipped_len(a, b, false), U = units_of(len);
+  while (p.at >= before + (int64_t)U * per) {              // (ends: at < end <= all units)
     before += (int64_t)U * per;
     len = clipped_len(a, ++b, false);
     U = units_of(len);
   }
-  const int64_t rel = at - before;
-  const int seg = (int)(rel / U);
+  const int64_t rel = p.at - before;
+  const int seg = (int)quotient(rel, U);
   sg.b = b; sg.hk = seg / blocks; sg.block = seg % blocks; sg.len = len;
   sg.unit = (int)(rel - (int64_t)seg * U);
   sg.units = U;
-  sg.n = (int)min((int64_t)(U - sg.unit), end - at);
-  if (threadIdx.x == 0) { w.at = at + sg.n; w.before = before; w.b = b; }
+  sg.n = (int)min((int64_t)(U - sg.unit), end - p.at);
+  if (threadIdx.x == 0) w.place[(turn + 1) & 1] = {p.at + sg.n, before, b};
   return true;
+}
+// Sum of `v` over the threads before this one; `total`: over all of them.
+__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* scratch, int64_t& total) {
+  int64_t sum = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t up = __shfl_up_sync(0xffffffffu, sum, o);
+    if ((int)(threadIdx.x & 31) >= o) sum += up;
+  }
+  __syncthreads();
+  if ((threadIdx.x & 31) == 31) scratch[threadIdx.x >> 5] = sum;
+  __syncthreads();
+  total = 0;
+  for (int k = 0; k < (int)(blockDim.x >> 5); ++k) {
+    if (k < (int)(threadIdx.x >> 5)) sum += scratch[k];
+    total += scratch[k];
+  }
+  return sum - v;
 }
 __device__ __forceinline__ bool walk_begin(const CachedArgs& a, int least, Walk& w, Segment& sg) {
   const int per = segments_per_sequence(a);
-  int64_t mine = 0;
-  for (int b = threadIdx.x; b < a.B; b += blockDim.x) mine += units_of(clipped_len(a, b, blockIdx.x == 0));
-  const int64_t total = block_sum(mine, w.scratch) * per, run = run_of(total, gridDim.x, least);
-  const int64_t at = (int64_t)blockIdx.x * run;
-  if (at >= total) return false;
-  // the sequence that holds unit `at`: a scan over blockDim.x sequences at a time
-  int64_t before = 0;
-  for (int b0 = 0; b0 < a.B; b0 += blockDim.x) {
-    const int b = b0 + threadIdx.x;
-    const int64_t u = b < a.B ? (int64_t)units_of(clipped_len(a, b, false)) * per : 0;
-    int64_t sum = u;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t up = __shfl_up_sync(0xffffffffu, sum, o);
-      if ((int)(threadIdx.x & 31) >= o) sum += up;
-    }
-    __syncthreads();
-    if ((threadIdx.x & 31) == 31) w.scratch[threadIdx.x >> 5] = sum;
-    __syncthreads();
-    int64_t base = before, chunk = 0;
-    for (int k = 0; k < (int)(blockDim.x >> 5); ++k) {
-      if (k < (int)(threadIdx.x >> 5)) base += w.scratch[k];
-      chunk += w.scratch[k];
-    }
-    if (at >= base + sum - u && at < base + sum) {
-      w.b = b; w.before = base + sum - u; w.at = at; w.end = min(at + run, total);
-    }
-    before += chunk;
-    if (at < before) break;
+  int64_t total = 0;
+  if (a.B > (int)blockDim.x) {                             // more than one scan: all lengths once for their sum
+    int64_t mine = 0;
+    for (int b = threadIdx.x; b < a.B; b += blockDim.x) mine += units_of(clipped_len(a, b, false));
+    total = block_sum(mine, w.scratch) * per;
   }
-  return walk_next(a, w, sg);
+  int64_t before = 0;
+  for (int b0 = 0; b0 < a.B; b0 += blockDim.x) {           // the sequence that holds the run's first unit
+    const int b = b0 + threadIdx.x;
+    const int64_t u = b < a.B ? (int64_t)units_of(clipped_len(a, b, blockIdx.x == 0)) * per : 0;
+    int64_t all;
+    const int64_t base = before + block_scan(u, w.scratch, all);
+    if (a.B <= (int)blockDim.x) total = all;
+    const int64_t run = run_of(total, gridDim.x, least), at = (int64_t)blockIdx.x * run;
+    if (blockIdx.x > 0 && at >= total) return false;
+    if (u > 0 && at >= base && at < base + u) {
+      w.place[0] = {at, base, b};
+      w.end = min(at + run, total);
+    }
+    before += all;
+    if (at < before && blockIdx.x > 0) break;              // (the first CTA looks at every length, to report bad ones)
+  }
+  __syncthreads();
+  return total > 0 && walk_next(a, w, sg, 0);
 }
 // Where a share of a segment leaves its partial result, or null: the share is all of it.
 __device__ __forceinline__ float* segment_slot(const CachedArgs& a, const Segment& sg) {

@@ -238,7 +238,8 @@ __global__ void __launch_bounds__(kCachedThreads) cached_simt_kernel(const Cache
   __shared__ Walk walk;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   Segment sg;
-  for (bool more = walk_begin(a, least, walk, sg); more; more = walk_next(a, walk, sg)) {
+  int turn = 0;
+  for (bool more = walk_begin(a, least, walk, sg); more; more = walk_next(a, walk, sg, ++turn)) {
     const int rows = min(kRows, a.nq * G - sg.block * kRows);
     __syncthreads();
     for (int i = tid; i < rows * (d / 8); i += kCachedThreads) {
@@ -353,7 +354,7 @@ __global__ void __launch_bounds__(kCachedThreads) cached_simt_kernel(const Cache
 // One CTA per row of a segment: nothing to do if one CTA held the whole segment; zeros if the sequence is empty;
 // otherwise the partial rows of CTAs c0 .. c1 are brought to their common maximum and added, each warp a share of them in
 // ascending order, the warps' sums in the order of the warps.
-constexpr int kJoinThreads = 128;
+constexpr int kJoinThreads = 256;
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const CachedArgs a, int ctas, int least) {
   __shared__ int64_t scratch[33];
@@ -393,14 +394,32 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const CachedArgs a, 
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   const float use = m == -INFINITY ? 0.f : m;
   float l = 0.f, x[8] = {};                                // columns lane + 32 j
-#pragma unroll 4
-  for (int i = warp; i < n; i += kJoinThreads / 32) {
-    const float* s = slot(i);
-    const float w = exp2f(tc::ld_after_wait(s + r) - use);
-    l = fmaf(w, tc::ld_after_wait(s + kRows + r), l);
+  // a batch of partial rows per turn, all its loads in flight together
+  constexpr int kBatch = 4;
+  for (int i0 = warp; i0 < n; i0 += kBatch * (kJoinThreads / 32)) {
+    float top[kBatch], sum[kBatch], part[kBatch][8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (lane + 32 * j < d && w != 0.f) x[j] = fmaf(w, tc::ld_after_wait(s + 2 * kRows + r * d + lane + 32 * j), x[j]);
+    for (int k = 0; k < kBatch; ++k) {
+      const int i = i0 + k * (kJoinThreads / 32);
+      top[k] = -INFINITY;
+      sum[k] = 0.f;
+      if (i >= n) continue;
+      const float* s = slot(i);
+      top[k] = tc::ld_after_wait(s + r);
+      sum[k] = tc::ld_after_wait(s + kRows + r);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (lane + 32 * j < d) part[k][j] = tc::ld_after_wait(s + 2 * kRows + r * d + lane + 32 * j);
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const float w = exp2f(top[k] - use);
+      if (w == 0.f) continue;
+      l = fmaf(w, sum[k], l);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (lane + 32 * j < d) x[j] = fmaf(w, part[k][j], x[j]);
+    }
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) sums[warp][lane + 32 * j] = x[j];

@@ -15,14 +15,19 @@
 //   keys    s = sum_g step_g <q_g, c_g> + lo_g sum(q_g):  one accumulator per group of 32 dimensions.
 //   values  o_g += (p step_g) c + (p lo_g):  the weight is multiplied by each group's step before it is rounded to
 //           bfloat16; p lo_g is summed per row and group in float32.
-//   A pair of codes becomes a pair of bfloat16 by one AND-OR: 0x4300 | c is 128 + c.  The 128 is taken out again: of s
-//   with lo_g - 128 step_g in the place of lo_g, of o by a product of the same rounded weights with a constant -128, so
-//   that nothing of a rounding is left behind.
+//   Keys: a code in the low bits of a 16-bit half is a subnormal number of half precision, c 2^-24, one place further up
+//   c 2^-20; the tensor cores take those exactly, and the queries (brought to 2^14 by a power of two for their row, and
+//   by 2^-4 where the code stands higher) lose nothing that a float32 sum would keep.  An AND makes a pair of codes.
+//   Values: the weights p step_g have a range of their own and stay bfloat16; an AND-OR makes 0x4300 | c, which is 128 + c,
+//   of a code, and a product of the same rounded weights with a constant -128 takes the 128 out again, so that nothing
+//   of a rounding is left behind.
 // float32: rows by tf32 products of two parts each (the lowest product left out: 2^-22 of a term); 4 bits with float32
-// queries by three bfloat16 parts of the query and of the weight, which are all of their 24 bits.
+// queries by three parts of the query (half precision) and of the weight (bfloat16), which are all of their 24 bits.
 //
 // The running maximum of a row is raised only when a logit exceeds it by 2^8 (weights stay below 2^8, sums far inside
 // float32): most units need a vote instead of shuffles and rescaling.
+#include <cuda_fp16.h>
+
 #include "avq_exact.cuh"
 #include "avq_tc_common.cuh"
 
@@ -48,8 +53,8 @@ template <int MODE, int D, int NT, int PARTS> __host__ __device__ constexpr size
 }
 
 __device__ __forceinline__ uint32_t swizzle(int r) { return ((r & 1) << 2) | (r & 2) | ((r >> 2) & 1); }
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {   // the rest of 16 bytes: zeros
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -60,36 +65,51 @@ __device__ __forceinline__ float ex2(float x) {
   return r;
 }
 __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {   // from zero
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
 __device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at));
 }
 __device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at));
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {   // an 8 x 8 matrix of 16-bit values, a pair per lane
   uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
 }
 __device__ __forceinline__ uint4 lds128(uint32_t at) {
   uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
   return v;
 }
 __device__ __forceinline__ uint2 lds64(uint32_t at) {
   uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
   return v;
 }
 template <int N> __device__ __forceinline__ void lds_words(uint32_t (&w)[N], uint32_t at) {   // N = 2 or 4
@@ -102,7 +122,13 @@ template <int N> __device__ __forceinline__ void lds_words(uint32_t (&w)[N], uin
   }
 }
 // 128 + c of the codes at bits 4 i of both halves
-__device__ __forceinline__ uint32_t codes_at(uint32_t w, int i) { return ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u; }
+__device__ __forceinline__ uint32_t codes_at(uint32_t w, int i) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(w >> (4 * i)), "r"(0x000f000fu), "r"(0x43004300u));   // (a & b) | c
+  return r;
+}
+// c 2^-24 of the codes at bits 4 (i - i % 2) of both halves, c 2^-20 of those at bits 4 i (odd i)
+__device__ __forceinline__ uint32_t subnormal_codes(uint32_t w, int i) { return (w >> (8 * (i >> 1))) & ((i & 1) ? 0x00f000f0u : 0x000f000fu); }
 __device__ __forceinline__ float tf32_high(float x) { return __uint_as_float(__float_as_uint(x) & 0xffffe000u); }
 __device__ __forceinline__ float low_f(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float high_f(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
@@ -113,6 +139,14 @@ __device__ __forceinline__ void three_parts(float x, float y, uint32_t (&p)[3]) 
     p[i] = pack_bf16(x, y);
     x -= low_f(p[i]);
     y -= high_f(p[i]);
+  }
+}
+__device__ __forceinline__ void three_f16_parts(float x, float y, uint32_t (&p)[3]) {
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    p[i] = pack_f16(x, y);
+    x -= __half2float(__ushort_as_half((unsigned short)p[i]));
+    y -= __half2float(__ushort_as_half((unsigned short)(p[i] >> 16)));
   }
 }
 
@@ -126,9 +160,11 @@ struct Warp {
 
   float O[D / 16][NT][4];        // C fragments of O^T: columns (rows of the product) 8 nt + 2 t, + 1
   float m[NT][2], l[NT][2];      // maximum (the same in the 8 lanes of a column), this lane's share of the sum
+  float limit[NT][2], sub[NT][2];   // the logit that raises the maximum, what is taken off scale * logit (powers of two)
   float off[NT][2][MODE == kQ4 ? kGroups : 1];   // sum p lo_g, this lane's share
   uint32_t q[MODE == kBf16 || (MODE == kQ4 && PARTS == 1) ? D / 16 : 1][NT][2];
   float qsum[MODE == kQ4 ? kGroups : 1][NT][2];
+  float qback[NT][2];            // (4 bits) what the products with the codes are multiplied by: 2^24 and the row's power of two
   int lim[NT][2];                // tokens that the column's query sees
 
   __device__ __forceinline__ void clear() {
@@ -142,47 +178,57 @@ struct Warp {
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        m[n][e] = -INFINITY;
-        l[n][e] = 0.f;
+        m[n][e] = limit[n][e] = -INFINITY;
+        l[n][e] = sub[n][e] = 0.f;
 #pragma unroll
         for (int w = 0; w < (MODE == kQ4 ? kGroups : 1); ++w) off[n][e][w] = 0.f;
       }
   }
 
-  // Copies of one unit's rows into `dst` (shared), `rows` of them (0: none, zeros instead).
-  static __device__ __forceinline__ void fetch(uint32_t dst, const CachedArgs& a, int page, int hk, int row0, int rows, int lane) {
-    const int64_t head = (int64_t)max(page, 0) * a.Hk + hk;
-    if (page < 0) rows = 0;
+  // Where a key head's rows are: this lane's first copy of the first page, bytes from page to page.
+  struct Source {
+    const char *k, *v, *pairs;
+    int64_t page_bytes;
+  };
+  static __device__ __forceinline__ Source source_of(const CachedArgs& a, int hk, int lane) {
+    Source r;
+    constexpr int row = MODE == kQ4 ? D / 2 + D / 8 : D * (MODE == kF32 ? 4 : 2);
+    const int64_t head = (int64_t)a.page * row;
+    r.page_bytes = head * a.Hk;
+    r.k = static_cast<const char*>(a.keys) + hk * head + 16 * lane;
+    r.v = static_cast<const char*>(a.values) + hk * head + 16 * lane;
     if constexpr (MODE == kQ4) {
-      const char* k = static_cast<const char*>(a.keys) + head * q4_page_bytes(a.page, D);
-      const char* v = static_cast<const char*>(a.values) + head * q4_page_bytes(a.page, D);
-      constexpr int per = D / 32, count = kUnit * per;   // 16-byte chunks of a code row, of the unit
+      constexpr int pairs = kUnit * D / 8 / 16;            // 16-byte chunks of a unit's (lo, step) pairs: 16 or 8
+      r.pairs = (lane < pairs ? r.k : r.v) + a.page * (D / 2) + 16 * (lane % pairs) - 16 * lane;
+    }
+    return r;
+  }
+  // Copies of one unit, the `in_page`-th 16 rows of a page, into `dst` (shared).  Rows behind a sequence's last come along:
+  // what they hold is kept out of the products.
+  static __device__ __forceinline__ void fetch(uint32_t dst, const Source& src, int page, int in_page, int lane) {
+    const int64_t at_page = (int64_t)page * src.page_bytes;
+    if constexpr (MODE == kQ4) {
+      constexpr int per = D / 32, count = kUnit * per;     // 16-byte chunks of a code row, of the unit
+      const char *k = src.k + at_page + in_page * (kUnit * D / 2), *v = src.v + at_page + in_page * (kUnit * D / 2);
 #pragma unroll
       for (int i0 = 0; i0 < count; i0 += 32) {
         const int i = i0 + lane, r = i / per, c = i % per;
         const uint32_t at = dst + 16 * (r * per + (D == 128 ? c ^ ((r >> 1) & 3) : c ^ ((r >> 2) & 1)));
-        const int n = r < rows ? 16 : 0;
-        cp_async16(at, k + row0 * (D / 2) + 16 * i, n);
-        cp_async16(at + kV, v + row0 * (D / 2) + 16 * i, n);
+        cp_async16(at, k + 16 * i0);
+        cp_async16(at + kV, v + 16 * i0);
       }
-      constexpr int pairs = kUnit * D / 8 / 16;          // chunks of (lo, step) pairs: 16 or 8
-      if (lane < 2 * pairs) {
-        const int i = lane % pairs;
-        const char* src = (lane < pairs ? k : v) + a.page * (D / 2) + row0 * (D / 8) + 16 * i;
-        const int n = min(16, max(0, rows * (D / 8) - 16 * i));
-        cp_async16(dst + (lane < pairs ? kKPairs : kVPairs) + 16 * i, src, n);
-      }
+      constexpr int pairs = kUnit * D / 8 / 16;
+      if (2 * pairs == 32 || lane < 2 * pairs)
+        cp_async16(dst + (lane < pairs ? kKPairs : kVPairs) + 16 * (lane % pairs), src.pairs + at_page + in_page * (kUnit * D / 8));
     } else {
       constexpr int row = kChunks * 16;
-      const char* k = static_cast<const char*>(a.keys) + (head * a.page + row0) * row;
-      const char* v = static_cast<const char*>(a.values) + (head * a.page + row0) * row;
-#pragma unroll 8
+      const char *k = src.k + at_page + in_page * (kUnit * row), *v = src.v + at_page + in_page * (kUnit * row);
+#pragma unroll
       for (int i0 = 0; i0 < kUnit * kChunks; i0 += 32) {
         const int i = i0 + lane, r = i / kChunks, c = i % kChunks;
         const uint32_t at = dst + r * row + 16 * (c ^ swizzle(r));
-        const int n = r < rows ? 16 : 0;
-        cp_async16(at, k + 16 * i, n);
-        cp_async16(at + kV, v + 16 * i, n);
+        cp_async16(at, k + 16 * i0);
+        cp_async16(at + kV, v + 16 * i0);
       }
     }
   }
@@ -205,33 +251,45 @@ struct Warp {
           q[k][n][1] = ok ? *reinterpret_cast<const uint32_t*>(src + 16 * k + 2 * t + 8) : 0u;
         }
       } else if constexpr (MODE == kQ4) {
-        float part[kGroups];
+        float part[kGroups], x[kGroups][8], most = 0.f;
 #pragma unroll
         for (int w = 0; w < kGroups; ++w) {
-          float x[8];
-          if (ok) load8(src + 32 * w + 8 * t, x);
-          else {
+          if (ok) load8(src + 32 * w + 8 * t, x[w]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = 0.f;
+          for (int i = 0; i < 8; ++i) {
+            if (!ok) x[w][i] = 0.f;
+            most = fmaxf(most, fabsf(x[w][i]));
           }
-          part[w] = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+          part[w] = ((x[w][0] + x[w][1]) + (x[w][2] + x[w][3])) + ((x[w][4] + x[w][5]) + (x[w][6] + x[w][7]));
+        }
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        // the power of two that brings the row's largest element to 2^14 .. 2^15 (an infinity stays one)
+        const int e = min(max((int)(__float_as_uint(most) >> 23), 27), 244);
+        const float up = __uint_as_float((uint32_t)(268 - e) << 23);          // 2^(141 - e), e biased
+        const float back = __uint_as_float((uint32_t)(e + 10) << 23);        // 2^(e - 141 + 24)
+#pragma unroll
+        for (int w = 0; w < kGroups; ++w)
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
+            const float u0 = x[w][2 * s] * up, u1 = x[w][2 * s + 4] * up, v0 = x[w][2 * s + 1] * up * 0.0625f, v1 = x[w][2 * s + 5] * up * 0.0625f;
             if constexpr (PARTS == 1) {
-              q[2 * w + s][n][0] = pack_bf16(x[2 * s], x[2 * s + 4]);
-              q[2 * w + s][n][1] = pack_bf16(x[2 * s + 1], x[2 * s + 5]);
+              q[2 * w + s][n][0] = pack_f16(u0, u1);
+              q[2 * w + s][n][1] = pack_f16(v0, v1);
             } else if (write) {
               uint32_t p0[3], p1[3];
-              three_parts(x[2 * s], x[2 * s + 4], p0);
-              three_parts(x[2 * s + 1], x[2 * s + 5], p1);
+              three_f16_parts(u0, u1, p0);
+              three_f16_parts(v0, v1, p1);
               uint2* to = reinterpret_cast<uint2*>(shared) + ((2 * w + s) * NT + n) * 3 * 32 + lane;
 #pragma unroll
               for (int i = 0; i < 3; ++i) to[32 * i] = make_uint2(p0[i], p1[i]);
             }
           }
-        }
+        qback[n][0] = __shfl_sync(0xffffffffu, back, 8 * t);
+        qback[n][1] = __shfl_sync(0xffffffffu, back, 8 * t + 4);
 #pragma unroll
         for (int w = 0; w < kGroups; ++w) {              // sums of groups, moved to the lanes of their columns
+          part[w] *= 1.f / back;                           // (a power of two)
           part[w] += __shfl_xor_sync(0xffffffffu, part[w], 1);
           part[w] += __shfl_xor_sync(0xffffffffu, part[w], 2);
           qsum[w][n][0] = __shfl_sync(0xffffffffu, part[w], 8 * t);
@@ -284,33 +342,38 @@ struct Warp {
       for (int w = 0; w < kGroups; ++w) {
         float c[NT][4];
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) c[n][e] = 0.f;
-#pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const uint32_t f[4] = {codes_at(x[w], 2 * k), codes_at(y[w], 2 * k), codes_at(x[w], 2 * k + 1), codes_at(y[w], 2 * k + 1)};
+          const uint32_t f[4] = {subnormal_codes(x[w], 2 * k), subnormal_codes(y[w], 2 * k), subnormal_codes(x[w], 2 * k + 1),
+                                 subnormal_codes(y[w], 2 * k + 1)};
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
             if constexpr (PARTS == 1) {
-              mma_bf16(c[n], f, q[2 * w + k][n][0], q[2 * w + k][n][1]);
+              if (k == 0) mma_f16_first(c[n], f, q[2 * w][n][0], q[2 * w][n][1]);
+              else mma_f16(c[n], f, q[2 * w + 1][n][0], q[2 * w + 1][n][1]);
             } else {
               const uint2* from = reinterpret_cast<const uint2*>(shared) + ((2 * w + k) * NT + n) * 3 * 32 + lane;
 #pragma unroll
-              for (int i = 2; i >= 0; --i) mma_bf16(c[n], f, from[32 * i].x, from[32 * i].y);
+              for (int i = 2; i >= 0; --i) {
+                if (k == 0 && i == 2) mma_f16_first(c[n], f, from[32 * i].x, from[32 * i].y);
+                else mma_f16(c[n], f, from[32 * i].x, from[32 * i].y);
+              }
             }
           }
         }
-        const float sx = high_f(px[w]), sy = high_f(py[w]);
-        const float lx = fmaf(-128.f, sx, low_f(px[w])), ly = fmaf(-128.f, sy, low_f(py[w]));
+        const float sx = high_f(px[w]), sy = high_f(py[w]), lx = low_f(px[w]), ly = low_f(py[w]);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            s[n][e] = fmaf(sx, c[n][e], fmaf(lx, qsum[w][n][e], s[n][e]));
-            s[n][2 + e] = fmaf(sy, c[n][2 + e], fmaf(ly, qsum[w][n][e], s[n][2 + e]));
+            // (the query's power of two is in qsum too: taken back at the end)
+            s[n][e] = fmaf(sx, c[n][e], w == 0 ? lx * qsum[w][n][e] : fmaf(lx, qsum[w][n][e], s[n][e]));
+            s[n][2 + e] = fmaf(sy, c[n][2 + e], w == 0 ? ly * qsum[w][n][e] : fmaf(ly, qsum[w][n][e], s[n][2 + e]));
           }
       }
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[n][e] *= qback[n][e & 1];
     } else {
 #pragma unroll 4
       for (int c = 0; c < D / 16; ++c) {
@@ -339,8 +402,9 @@ struct Warp {
   }
 
   // O^T += V^T P^T for one unit.  p: weights in the layout of the logits.
-  // skip: tokens from `seen` on do not exist for this product (raw rows: their values are made zero).
-  __device__ __forceinline__ void values(uint32_t at, const float (&p)[NT][4], int seen, bool skip, int lane) {
+  // SKIP: tokens from `seen` on do not exist for this product (raw rows: their values are made zero).
+  template <bool SKIP>
+  __device__ __forceinline__ void values(uint32_t at, const float (&p)[NT][4], int seen, int lane) {
     const int g = lane >> 2, t = lane & 3;
     if constexpr (MODE == kBf16) {
       uint32_t b[NT][2];
@@ -356,7 +420,7 @@ struct Warp {
       for (int i = 0; i < D / 16; ++i) {
         uint32_t v[4];
         ldmatrix4_trans(v, at + kV + r * (2 * D) + 16 * ((2 * i + c) ^ swizzle(r)));
-        if (skip) { v[0] &= keep[0]; v[1] &= keep[0]; v[2] &= keep[1]; v[3] &= keep[1]; }
+        if (SKIP) { v[0] &= keep[0]; v[1] &= keep[0]; v[2] &= keep[1]; v[3] &= keep[1]; }
 #pragma unroll
         for (int n = 0; n < NT; ++n) mma_bf16(O[i][n], v, b[n][0], b[n][1]);
       }
@@ -383,12 +447,14 @@ struct Warp {
           for (int e = 0; e < 2; ++e) {
             x[e] = p[n][e] * sx;
             x[2 + e] = p[n][2 + e] * sy;
-            float a = p[n][e] * lx, c = p[n][2 + e] * ly;
-            if (skip) {                                  // (a token that is not seen may have any step and lo)
-              if (p[n][e] == 0.f) { x[e] = 0.f; a = 0.f; }
-              if (p[n][2 + e] == 0.f) { x[2 + e] = 0.f; c = 0.f; }
+            if (!SKIP) {
+              off[n][e][w] = fmaf(p[n][e], lx, fmaf(p[n][2 + e], ly, off[n][e][w]));
+            } else {                                     // (a token that is not seen may have any step and lo)
+              if (p[n][e] == 0.f) x[e] = 0.f;
+              else off[n][e][w] = fmaf(p[n][e], lx, off[n][e][w]);
+              if (p[n][2 + e] == 0.f) x[2 + e] = 0.f;
+              else off[n][e][w] = fmaf(p[n][2 + e], ly, off[n][e][w]);
             }
-            off[n][e][w] += a + c;
           }
           if constexpr (PARTS == 1) {
             b[n][0][0] = transpose8(pack_bf16(x[0], x[1]));
@@ -434,7 +500,7 @@ struct Warp {
         for (int j = 0; j < 4; ++j) {
           const int r = t + 4 * j;
           const uint4 u = lds128(at + kV + r * (4 * D) + 16 * ((8 * c + g) ^ swizzle(r)));
-          const bool keep = !skip || r < seen;
+          const bool keep = !SKIP || r < seen;
           v[j][0] = keep ? u.x : 0u; v[j][1] = keep ? u.y : 0u; v[j][2] = keep ? u.z : 0u; v[j][3] = keep ? u.w : 0u;
         }
 #pragma unroll
@@ -459,7 +525,7 @@ struct Warp {
     }
   }
 
-  // One unit: tokens from `token` on, the first `rows` of them in shared memory at `at`.
+  // One unit: tokens from `token` on, of which the first `rows` count, in shared memory at `at`.
   __device__ __forceinline__ void unit(uint32_t at, const uint4* shared, int token, int rows, int len, int nq, float c, int lane) {
     const int g = lane >> 2;
     float s[NT][4];
@@ -481,7 +547,7 @@ struct Warp {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         top[n][e] = fmaxf(s[n][e], s[n][2 + e]);
-        raise |= (top[n][e] - m[n][e]) * c > kRaise || (m[n][e] == -INFINITY && top[n][e] > -INFINITY);
+        raise |= top[n][e] > limit[n][e];
       }
     if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
@@ -494,6 +560,8 @@ struct Warp {
           x = fmaxf(x, m[n][e]);
           const float f = x == -INFINITY ? 1.f : ex2((m[n][e] - x) * c);
           m[n][e] = x;
+          limit[n][e] = x + kRaise / c;
+          sub[n][e] = x == -INFINITY ? 0.f : x * c;
           l[n][e] *= f;
 #pragma unroll
           for (int w = 0; w < (MODE == kQ4 ? kGroups : 1); ++w) off[n][e][w] *= f;
@@ -505,13 +573,17 @@ struct Warp {
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float use = m[n][e] == -INFINITY ? 0.f : m[n][e] * c;
-        s[n][e] = ex2(fmaf(s[n][e], c, -use));
-        s[n][2 + e] = ex2(fmaf(s[n][2 + e], c, -use));
+        s[n][e] = ex2(fmaf(s[n][e], c, -sub[n][e]));
+        s[n][2 + e] = ex2(fmaf(s[n][2 + e], c, -sub[n][e]));
         l[n][e] += s[n][e] + s[n][2 + e];
       }
-    if (MODE == kQ4 || nq == 1 || !edge) {
-      values(at, s, kUnit, MODE == kQ4 && edge, lane);
+    if (!edge) {
+      values<false>(at, s, kUnit, lane);
+      return;
+    }
+
+    if (MODE == kQ4 || nq == 1) {
+      values<true>(at, s, rows, lane);
       return;
     }
     // Some queries see fewer of these tokens than others: one product per distinct number, from values that are zero
@@ -538,7 +610,7 @@ struct Warp {
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int e = 0; e < 4; ++e) keep[i][n][e] = O[i][n][e];
-      values(at, s, next, true, lane);
+      values<true>(at, s, next, lane);
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -568,43 +640,59 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<MODE, D, NT>()) cached_k
   uint4* queries = reinterpret_cast<uint4*>(smem + (size_t)kWarps * S * W::kUnitBytes);
   const uint32_t ring = tc::smem_u32(smem) + warp * S * W::kUnitBytes;
   const float c = a.scale * kLog2e;
-  const int G = a.H / a.Hk;
+  const int G = a.H / a.Hk, per_page = a.page / kUnit, shift = per_page > 1 ? 32 - __clz(per_page - 1) : 0;
   W w;
   Segment sg;
-  for (bool more = walk_begin(a, least, walk, sg); more; more = walk_next(a, walk, sg)) {
+  int turn = 0;
+  for (bool more = walk_begin(a, least, walk, sg); more; more = walk_next(a, walk, sg, ++turn)) {
     const int first = sg.unit + warp, end = sg.unit + sg.n;
     const int mine = first < end ? (end - first + kWarps - 1) / kWarps : 0;
+    // Where this warp's units are, 32 of them at a time, one in each lane: physical page and place in it in one word (fewer
+    // than 2^28 of them), the next 32 read ahead.  A page that is not there is read as the first one: none of its rows count.
+    const typename W::Source src = W::source_of(a, sg.hk, lane);
     const int32_t* table = a.table + (int64_t)sg.b * a.table_pages;
-    auto page_at = [&](int k) {                            // physical page of this warp's k-th unit
-      return k < mine ? table[(first + k * kWarps) * kUnit / a.page] : 0;
+    auto place_of = [&](int k) {
+      if (k >= mine) return 0;
+      const int u = first + k * kWarps, entry = u / per_page, page = table[entry];
+      return page < 0 || page >= a.pages ? -1 : page << shift | (u - entry * per_page);
     };
-    auto fetch = [&](int k, int page) {
-      if (k < mine) {
-        const int token = (first + k * kWarps) * kUnit;
-        const bool ok = page >= 0 && page < a.pages;
-        if (!ok && lane == 0) report(a.status, DEV_BAD_INDEX);
-        W::fetch(ring + (k % S) * W::kUnitBytes, a, ok ? page : -1, sg.hk, token % a.page, min(kUnit, sg.len - token), lane);
+    int places = place_of(lane), then_places = 0, fetched = 0;
+    uint32_t bad = 0;                                      // of the units in flight, those whose page is not there
+    auto fetch = [&](int slot) {
+      bad <<= 1;
+      if (fetched < mine) {
+        if ((fetched & 31) == 0) {
+          if (fetched > 0) places = then_places;
+          then_places = place_of(fetched + 32 + lane);
+        }
+        int place = __shfl_sync(0xffffffffu, places, fetched & 31);
+        if (place < 0) {
+          bad |= 1;
+          place = 0;
+          if (lane == 0) report(a.status, DEV_BAD_INDEX);
+        }
+        W::fetch(ring + slot * W::kUnitBytes, src, place >> shift, place & ((1 << shift) - 1), lane);
+        ++fetched;
       }
       cp_async_commit();
     };
-    int ahead = 0;
 #pragma unroll
-    for (int k = 0; k < S - 1; ++k) fetch(k, page_at(k));
-    ahead = page_at(S - 1);
+    for (int k = 0; k < S - 1; ++k) fetch(k);
     w.clear();
     if (MODE == kF32 || PARTS == 3) __syncthreads();       // (the segment before is done with the shared queries)
     w.template load_queries<T>(a, sg, queries, warp == 0, lane);
     if (MODE == kF32 || PARTS == 3) __syncthreads();
+    int now = 0, next = S - 1, token = first * kUnit;
     for (int k = 0; k < mine; ++k) {
       cp_async_wait<S - 2>();
       __syncwarp();
-      const int token = (first + k * kWarps) * kUnit;
-      const int page = page_at(k);
-      const int rows = page >= 0 && page < a.pages ? min(kUnit, sg.len - token) : 0;
-      fetch(k + S - 1, ahead);
-      ahead = page_at(k + S);
-      w.unit(ring + (k % S) * W::kUnitBytes, queries, token, rows, sg.len, a.nq, c, lane);
+      fetch(next);
+      const int rows = (bad >> (S - 1)) & 1 ? 0 : min(kUnit, sg.len - token);
+      w.unit(ring + now * W::kUnitBytes, queries, token, rows, sg.len, a.nq, c, lane);
       __syncwarp();
+      token += kWarps * kUnit;
+      now = now + 1 == S ? 0 : now + 1;
+      next = next + 1 == S ? 0 : next + 1;
     }
     cp_async_wait<0>();
     // ---- the warps' results added: maxima, sums and outputs through shared memory, in the order of the warps
