@@ -362,37 +362,31 @@ def forward_static(Q, K, V, Cp, Cc, P: int, block_q: int, scale=None, flags: int
 
 
 # ---------------------------------------------------------------- exact attention
-def _rows(name, t, heads, d, dtype, T=None):
+# (These run at every call of a model's layer: few Python operations on the way where all is well.)
+def _rows(name, t, heads, d, dtype, T):
     """A tensor of T rows, [T, heads, d] with dense heads and rows any distance apart; returns that distance."""
-    if t.dim() != 3 or tuple(t.shape[1:]) != (heads, d) or (T is not None and t.shape[0] != T):
-        raise ValueError(f"{name} must be [{'T' if T is None else T}, {heads}, {d}], not {tuple(t.shape)}")
-    if t.dtype != dtype:
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != T or shape[1] != heads or shape[2] != d:
+        raise ValueError(f"{name} must be [{T}, {heads}, {d}], not {tuple(shape)}")
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    if t.shape[0] and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != d)):
+    row, head, one = t.stride()
+    if T and (one != 1 or (head != d and heads > 1)):
         raise ValueError(f"the heads of a row of {name} must be dense")
     # (the stride of a single row, or of none, is anybody's: any usable one will do)
-    return t.stride(0) if t.shape[0] > 1 else heads * d
+    return row if T > 1 else heads * d
 
 
-def _ints(name, t, *shape):
-    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+def _ints(name, t, shape):
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape}, not {t.dtype} {tuple(t.shape)}")
 
 
-def _here(**ts):
-    """All tensors are on the current CUDA device, whose current stream the call goes to."""
-    at = None
-    for name, t in ts.items():
-        if t is None:
-            continue
-        if t.is_cuda and at is None:
-            at = torch._C._cuda_getDevice()
-        if not t.is_cuda or t.get_device() != at:
-            raise ValueError(f"{name} must be on the current CUDA device, not {t.device}")
-
-
-def _addr(t):
-    return 0 if t is None else t.data_ptr()
+def _here(at, *ts):
+    """All tensors (None: no tensor) are on device `at`, the current one, whose current stream the call goes to."""
+    for t in ts:
+        if t is not None and t.get_device() != at:
+            raise ValueError(f"tensors must be on the current CUDA device, not on {t.device}")
 
 
 class ExactAttention:
@@ -413,29 +407,35 @@ class ExactAttention:
         if n == 0:
             raise AvqError(lib().avq_prompt_attend(self.heads, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0) or 3,
                            "avq_prompt_workspace_bytes")
-        self.workspace = torch.zeros(n, dtype=torch.uint8, device=device)
+        self.workspace, self.bytes, self.sizes = torch.zeros(n, dtype=torch.uint8, device=device), n, (H, Hk, d)
 
     def __call__(self, Q, K, V, cu_q, cu_k=None, Y=None, lse=False):
-        h = self.heads
+        h, dtype = self.heads, self.dtype
+        H, Hk, d = self.sizes
         Tq, Tk, S = Q.shape[0], K.shape[0], cu_q.shape[0] - 1
-        qs, ks, vs = (_rows("Q", Q, h.H, h.d, self.dtype), _rows("K", K, h.Hk, h.d, self.dtype),
-                      _rows("V", V, h.Hk, h.d, self.dtype, Tk))
         if S < 0 or (cu_k is None and Tq != Tk):
             raise ValueError("cu_q must hold S + 1 bounds, and cu_k too where queries and keys differ in number")
-        _ints("cu_q", cu_q, S + 1)
+        qs, ks, vs = (_rows("Q", Q, H, d, dtype, Tq), _rows("K", K, Hk, d, dtype, Tk), _rows("V", V, Hk, d, dtype, Tk))
+        _ints("cu_q", cu_q, (S + 1,))
         if cu_k is not None:
-            _ints("cu_k", cu_k, S + 1)
-        _here(Q=Q, K=K, V=V, cu_q=cu_q, cu_k=cu_k, Y=Y, workspace=self.workspace)
+            _ints("cu_k", cu_k, (S + 1,))
+        at = torch._C._cuda_getDevice() if Q.is_cuda else -2
+        _here(at, Q, K, V, cu_q, cu_k, Y, self.workspace)
         if Y is None:
-            Y = torch.empty((Tq, h.H, h.d), dtype=self.dtype, device=Q.device)
-        ys = _rows("Y", Y, h.H, h.d, self.dtype, Tq)
-        L = torch.empty((Tq, h.H), dtype=torch.float32, device=Q.device) if lse else None
-        st = (_lib or lib()).avq_prompt_attend(h, _addr(Q), qs, _addr(K), ks, _addr(V), vs, _addr(cu_q), _addr(cu_k), S, Tq,
-                                               Tk, _addr(Y), ys, _addr(L), self.workspace.data_ptr(),
-                                               self.workspace.numel(), _raw_stream())
+            Y, ys = Q.new_empty((Tq, H, d)), H * d
+        else:
+            ys = _rows("Y", Y, H, d, dtype, Tq)
+        L = Q.new_empty((Tq, H), dtype=torch.float32) if lse else None
+        st = self._call(h, Q.data_ptr(), qs, K.data_ptr(), ks, V.data_ptr(), vs, cu_q.data_ptr(),
+                        None if cu_k is None else cu_k.data_ptr(), S, Tq, Tk, Y.data_ptr(), ys, L.data_ptr() if lse else None,
+                        self.workspace.data_ptr(), self.bytes, torch._C._cuda_getCurrentRawStream(at))
         if st != 0:
             raise AvqError(st, "avq_prompt_attend")
         return (Y, L) if lse else Y
+
+    @property
+    def _call(self):
+        return (_lib or lib()).avq_prompt_attend
 
     def check(self) -> None:
         """avq_check: raises if a kernel left something out (unusable bounds) or gave up on a wait."""
@@ -466,6 +466,7 @@ class PagedCache:
         if int(lib().avq_cache_bytes(self.desc)) == 0:
             raise AvqError(lib().avq_cache_read(self.desc, 0, 0, 0, 0, 0, 0, 0, 0) or 3, "avq_cache_bytes")
         self.header = torch.zeros(256, dtype=torch.uint8, device=keys.device)
+        self.sizes = (Hk, d)
 
     @classmethod
     def empty(cls, pages, page, Hk, d, dtype=torch.bfloat16, bits=None, device="cuda"):
@@ -476,31 +477,34 @@ class PagedCache:
         """avq_cache_append: K, V [T,Hk,d] to the rows ``slots`` (int32 [T], -1: none), K rotated by the positions ``pos``
         (int32 [T]) with the float32 tables ``cos``, ``sin`` [rows, dims/2].  With Q [T,H,d] returns the rotated queries (in a
         Q_out made here the rows of slot -1 are anything)."""
-        c = self.desc
-        T = K.shape[0]
-        ks, vs = _rows("K", K, c.Hk, c.d, self.dtype), _rows("V", V, c.Hk, c.d, self.dtype, T)
-        _ints("slots", slots, T)
+        dtype, (Hk, d), T = self.dtype, self.sizes, K.shape[0]
+        ks, vs = _rows("K", K, Hk, d, dtype, T), _rows("V", V, Hk, d, dtype, T)
+        _ints("slots", slots, (T,))
         rot = None
         if pos is not None:
-            _ints("pos", pos, T)
+            _ints("pos", pos, (T,))
             for name, t in (("cos", cos), ("sin", sin)):
-                if t is None or t.dtype != torch.float32 or t.dim() != 2 or not t.is_contiguous() or t.shape != cos.shape:
+                if t is None or t.dtype is not torch.float32 or len(t.shape) != 2 or not t.is_contiguous() or t.shape != cos.shape:
                     raise ValueError(f"{name} must be a contiguous float32 table [rows, dims/2]")
-            rot = AvqRotation(cos.data_ptr(), sin.data_ptr(), pos.data_ptr(), cos.shape[0], 2 * cos.shape[1], int(adjacent))
+            rot = AvqRotation(cos.data_ptr(), sin.data_ptr(), pos.data_ptr(), cos.shape[0], 2 * cos.shape[1], adjacent)
         elif cos is not None or sin is not None:
             raise ValueError("a rotation needs the positions")
         H = qs = os_ = 0
         if Q is not None:
             H = Q.shape[1]
-            qs = _rows("Q", Q, H, c.d, self.dtype, T)
+            qs = _rows("Q", Q, H, d, dtype, T)
             if Q_out is None:
-                Q_out = torch.empty((T, H, c.d), dtype=self.dtype, device=Q.device)
-            os_ = _rows("Q_out", Q_out, H, c.d, self.dtype, T)
+                Q_out, os_ = Q.new_empty((T, H, d)), H * d
+            else:
+                os_ = _rows("Q_out", Q_out, H, d, dtype, T)
         elif Q_out is not None:
             raise ValueError("Q_out without Q")
-        _here(K=K, V=V, slots=slots, pos=pos, cos=cos, sin=sin, Q=Q, Q_out=Q_out, keys=self.keys)
-        st = (_lib or lib()).avq_cache_append(c, _addr(K), ks, _addr(V), vs, _addr(slots), T, rot, _addr(Q), qs, H,
-                                              _addr(Q_out), os_, self.header.data_ptr(), _raw_stream())
+        at = torch._C._cuda_getDevice() if K.is_cuda else -2
+        _here(at, K, V, slots, pos, cos, sin, Q, Q_out, self.keys)
+        st = (_lib or lib()).avq_cache_append(self.desc, K.data_ptr(), ks, V.data_ptr(), vs, slots.data_ptr(), T, rot,
+                                              None if Q is None else Q.data_ptr(), qs, H,
+                                              None if Q is None else Q_out.data_ptr(), os_, self.header.data_ptr(),
+                                              torch._C._cuda_getCurrentRawStream(at))
         if st != 0:
             raise AvqError(st, "avq_cache_append")
         return Q_out
@@ -508,17 +512,20 @@ class PagedCache:
     def read(self, slots, K=None, V=None):
         """avq_cache_read: the rows ``slots`` back as (K, V) [T,Hk,d]; rows of -1 are left as they are (in tensors
         made here: anything)."""
-        c = self.desc
-        T = slots.shape[0]
-        _ints("slots", slots, T)
+        dtype, (Hk, d), T = self.dtype, self.sizes, slots.shape[0]
+        _ints("slots", slots, (T,))
+        at = torch._C._cuda_getDevice() if slots.is_cuda else -2
+        _here(at, slots, K, V, self.keys)
         if K is None:
-            K = torch.empty((T, c.Hk, c.d), dtype=self.dtype, device=slots.device)
+            K, ks = slots.new_empty((T, Hk, d), dtype=dtype), Hk * d
+        else:
+            ks = _rows("K", K, Hk, d, dtype, T)
         if V is None:
-            V = torch.empty((T, c.Hk, c.d), dtype=self.dtype, device=slots.device)
-        ks, vs = _rows("K", K, c.Hk, c.d, self.dtype, T), _rows("V", V, c.Hk, c.d, self.dtype, T)
-        _here(slots=slots, K=K, V=V, keys=self.keys)
-        st = (_lib or lib()).avq_cache_read(c, _addr(slots), T, _addr(K), ks, _addr(V), vs, self.header.data_ptr(),
-                                            _raw_stream())
+            V, vs = slots.new_empty((T, Hk, d), dtype=dtype), Hk * d
+        else:
+            vs = _rows("V", V, Hk, d, dtype, T)
+        st = (_lib or lib()).avq_cache_read(self.desc, slots.data_ptr(), T, K.data_ptr(), ks, V.data_ptr(), vs,
+                                            self.header.data_ptr(), torch._C._cuda_getCurrentRawStream(at))
         if st != 0:
             raise AvqError(st, "avq_cache_read")
         return K, V
@@ -538,25 +545,28 @@ class PagedCache:
     def attend(self, Q, table, lens, scale=None, flags=0, Y=None, lse=False, plan=None):
         """avq_cache_attend: the last queries Q [B*nq,H,d] of B sequences (``lens`` int32 [B] tokens in the pages ``table``
         int32 [B, n]) over the cache.  Returns Y, or (Y, lse).  ``plan``: what ``plan`` made, else one is made here."""
-        c = self.desc
         B = lens.shape[0]
         if plan is None:
             if B == 0 or Q.shape[0] % B:
                 raise ValueError("Q must hold the same number of rows for each of the sequences of lens")
             plan = self.plan(Q.shape[1], B, max(1, Q.shape[0] // B), scale, flags)
         heads, ws, pB, nq = plan
-        if B != pB or table.dim() != 2:
+        if B != pB or len(table.shape) != 2:
             raise ValueError(f"lens must be [{pB}] and table [{pB}, n]")
-        qs = _rows("Q", Q, heads.H, c.d, self.dtype, B * nq)
-        _ints("lens", lens, B)
-        _ints("table", table, B, table.shape[1])
+        H, d, dtype, T, pages = heads.H, self.sizes[1], self.dtype, B * nq, table.shape[1]
+        qs = _rows("Q", Q, H, d, dtype, T)
+        _ints("lens", lens, (B,))
+        _ints("table", table, (B, pages))
+        at = torch._C._cuda_getDevice() if Q.is_cuda else -2
+        _here(at, Q, table, lens, Y, self.keys, ws)
         if Y is None:
-            Y = torch.empty((B * nq, heads.H, c.d), dtype=self.dtype, device=Q.device)
-        ys = _rows("Y", Y, heads.H, c.d, self.dtype, B * nq)
-        _here(Q=Q, table=table, lens=lens, Y=Y, keys=self.keys, workspace=ws)
-        L = torch.empty((B * nq, heads.H), dtype=torch.float32, device=Q.device) if lse else None
-        st = (_lib or lib()).avq_cache_attend(heads, c, _addr(Q), qs, _addr(table), table.shape[1], _addr(lens), B, nq,
-                                              _addr(Y), ys, _addr(L), ws.data_ptr(), ws.numel(), _raw_stream())
+            Y, ys = Q.new_empty((T, H, d)), H * d
+        else:
+            ys = _rows("Y", Y, H, d, dtype, T)
+        L = Q.new_empty((T, H), dtype=torch.float32) if lse else None
+        st = (_lib or lib()).avq_cache_attend(heads, self.desc, Q.data_ptr(), qs, table.data_ptr(), pages, lens.data_ptr(), B, nq,
+                                              Y.data_ptr(), ys, L.data_ptr() if lse else None, ws.data_ptr(), ws.numel(),
+                                              torch._C._cuda_getCurrentRawStream(at))
         if st != 0:
             raise AvqError(st, "avq_cache_attend")
         return (Y, L) if lse else Y
