@@ -304,12 +304,15 @@ typedef struct {
  * cu_k[s+1]-1 (device int32 [S+1], nondecreasing; cu_k NULL: the same as cu_q).  Every query sees all keys of its
  * sequence, with AVQ_FLAG_CAUSAL query i of nq the keys j <= i + nk - nq (the queries are the last ones of the keys).
  *   Q [Tq,H,d]   K, V [Tk,Hk,d]   Y [Tq,H,d]   lse_out: optional float32 [Tq,H], log sum_j exp(scale <q,k_j>)
- *   workspace    avq_prompt_workspace_bytes() bytes: the header.
+ *   workspace    at least avq_prompt_workspace_bytes() bytes, its first 256 the header.  With avq_prompt_split_bytes() a call
+ *                of few queries over many keys (bfloat16 on the tensor cores) is split along the keys and its partial
+ *                results joined, in a fixed order; such calls that may overlap need workspaces of their own.
  * Rows of Y (and lse_out) that belong to no sequence stay as they were.  Keys a query does not see have no effect on
  * its row, whatever they and their values hold, infinities and NaN included.  A sequence whose bounds are not
  * 0 <= cu[s] <= cu[s+1] <= T is left out and reported by avq_check() as AVQ_ERR_INDEX.  A call with S or Tq of 0
  * launches nothing. */
 AVQ_API size_t avq_prompt_workspace_bytes(const avq_heads* heads);
+AVQ_API size_t avq_prompt_split_bytes(const avq_heads* heads);
 AVQ_API avq_status avq_prompt_attend(const avq_heads* heads, const void* Q, int64_t q_stride, const void* K,
                              int64_t k_stride, const void* V, int64_t v_stride, const int32_t* cu_q,
                              const int32_t* cu_k, int32_t S, int32_t Tq, int32_t Tk, void* Y, int64_t y_stride,

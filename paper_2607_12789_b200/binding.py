@@ -24,7 +24,7 @@ EXPORTS = ("avq_workspace_bytes", "avq_assign", "avq_aggregate", "avq_forward", 
            "avq_workspace_layout", "avq_check", "avq_status_string", "avq_version", "avq_forward_static",
            "avq_check_static", "avq_static_workspace_bytes", "avq_workspace_bytes_permuted",
            "avq_forward_permuted", "avq_codebook_update_workspace_bytes", "avq_codebook_update",
-           "avq_forward_tiled", "avq_prompt_workspace_bytes", "avq_prompt_attend", "avq_cache_bytes", "avq_cache_append",
+           "avq_forward_tiled", "avq_prompt_workspace_bytes", "avq_prompt_split_bytes", "avq_prompt_attend", "avq_cache_bytes", "avq_cache_append",
            "avq_cache_read", "avq_cache_attend_workspace_bytes", "avq_cache_attend")
 
 
@@ -97,6 +97,7 @@ def lib() -> ctypes.CDLL:
         L.avq_codebook_update.argtypes = [pp, vp, vp, vp, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         i64, ph, pc = ctypes.c_int64, ctypes.POINTER(AvqHeads), ctypes.POINTER(AvqCache)
         L.avq_prompt_workspace_bytes.restype, L.avq_prompt_workspace_bytes.argtypes = sz, [ph]
+        L.avq_prompt_split_bytes.restype, L.avq_prompt_split_bytes.argtypes = sz, [ph]
         L.avq_prompt_attend.restype = i32
         L.avq_prompt_attend.argtypes = [ph, vp, i64, vp, i64, vp, i64, vp, vp, i32, i32, i32, vp, i64, vp, vp, sz, vp]
         L.avq_cache_bytes.restype, L.avq_cache_bytes.argtypes = sz, [pc]
@@ -394,20 +395,22 @@ class ExactAttention:
 
     ``ExactAttention(H, Hk, d)(Q, K, V, cu_q, cu_k=None)`` takes Q [Tq,H,d], K, V [Tk,Hk,d] (rows may be views of a
     wider tensor) and the int32 bounds [S+1] of the sequences' queries and keys, and returns Y [Tq,H,d], with ``lse`` also
-    the log of every query's sum, float32 [Tq,H].  Rows outside all sequences are left as they are (in a Y made here: anything)."""
+    the log of every query's sum, float32 [Tq,H].  ``split``: keep room (20 or 40 MB) for the parts of calls of few queries
+    over many keys; calls that may overlap then need plans of their own.  Rows outside all sequences are left as they are (in a Y made here: anything)."""
 
-    def __init__(self, H, Hk, d, dtype=torch.bfloat16, scale=None, causal=True, flags=0, device="cuda"):
+    def __init__(self, H, Hk, d, dtype=torch.bfloat16, scale=None, causal=True, flags=0, device="cuda", split=True):
         code = {torch.float32: AVQ_F32, torch.bfloat16: AVQ_BF16}.get(dtype)
         if code is None:
             raise TypeError(f"unsupported dtype {dtype}")
         self.heads = AvqHeads(H, Hk, d, code, float(scale) if scale is not None else 1.0 / math.sqrt(d),
                               flags | (FLAG_CAUSAL if causal else 0))
         self.dtype = dtype
-        n = int(lib().avq_prompt_workspace_bytes(self.heads))
+        n = int((lib().avq_prompt_split_bytes if split else lib().avq_prompt_workspace_bytes)(self.heads))
         if n == 0:
             raise AvqError(lib().avq_prompt_attend(self.heads, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0) or 3,
                            "avq_prompt_workspace_bytes")
-        self.workspace, self.bytes, self.sizes = torch.zeros(n, dtype=torch.uint8, device=device), n, (H, Hk, d)
+        self.workspace, self.bytes, self.sizes = torch.empty(n, dtype=torch.uint8, device=device), n, (H, Hk, d)
+        self.workspace[:256].zero_()
 
     def __call__(self, Q, K, V, cu_q, cu_k=None, Y=None, lse=False):
         h, dtype = self.heads, self.dtype

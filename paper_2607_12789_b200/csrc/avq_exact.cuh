@@ -25,6 +25,7 @@ struct PromptArgs {
   int32_t causal;
   float scale;
   int32_t* status;
+  float* parts;                  // room for the partial results of split pieces, or null
 };
 
 struct CachedArgs {
@@ -312,6 +313,8 @@ avq_status cache_read(const ReadArgs& a, int dtype, int bits, cudaStream_t st);
 avq_status simt_prompt(const PromptArgs& a, int dtype, cudaStream_t st);
 avq_status simt_cached(const CachedArgs& a, int dtype, int bits, cudaStream_t st);
 avq_status tc_prompt(const PromptArgs& a, cudaStream_t st);
+constexpr int kPromptCtas = 148;                           // (more SMs than that are not asked for)
+size_t tc_prompt_part_bytes(int d);
 avq_status tc_cached(const CachedArgs& a, int dtype, int bits, cudaStream_t st);
 avq_status join(const CachedArgs& a, int dtype, int ctas, int least, cudaStream_t st);
 

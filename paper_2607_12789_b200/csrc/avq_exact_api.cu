@@ -75,6 +75,11 @@ extern "C" {
 
 size_t avq_prompt_workspace_bytes(const avq_heads* heads) { return validate_prompt(heads) == AVQ_OK ? 256 : 0; }
 
+size_t avq_prompt_split_bytes(const avq_heads* heads) {
+  if (validate_prompt(heads) != AVQ_OK) return 0;
+  return 256 + (heads->dtype == AVQ_BF16 && tensor_path(*heads) ? tc_prompt_part_bytes(heads->d) : 0);
+}
+
 avq_status avq_prompt_attend(const avq_heads* heads, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
                              const void* V, int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k, int32_t S,
                              int32_t Tq, int32_t Tk, void* Y, int64_t y_stride, float* lse_out, void* workspace,
@@ -94,7 +99,9 @@ avq_status avq_prompt_attend(const avq_heads* heads, const void* Q, int64_t q_st
   AVQ_TRY(validate_header(workspace));
   if (S > (1 << 20)) return AVQ_ERR_UNSUPPORTED;
   const PromptArgs a = {Q, K, V, Y, lse_out, cu_q, cu_k, q_stride, k_stride, v_stride, y_stride, h.H, h.Hk, h.d, S, Tq, Tk,
-                        (h.flags & AVQ_FLAG_CAUSAL) ? 1 : 0, h.scale, static_cast<int32_t*>(workspace)};
+                        (h.flags & AVQ_FLAG_CAUSAL) ? 1 : 0, h.scale, static_cast<int32_t*>(workspace),
+                        workspace_bytes > 256 && workspace_bytes >= avq_prompt_split_bytes(heads)
+                            ? reinterpret_cast<float*>(static_cast<char*>(workspace) + 256) : nullptr};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return h.dtype == AVQ_BF16 && tensor_path(h) ? tc_prompt(a, st) : simt_prompt(a, h.dtype, st);
 }

@@ -7,11 +7,12 @@
 // the rows that it can.  Roles by warp:
 //   0-3, 4-7  one tile each, a thread per row: logits out of tensor memory, maximum, weights back as bfloat16 in their
 //             place, sum; at the end the outputs out of tensor memory
-//   8         loads (TMA): the two tiles of queries, then keys and values in turn through a ring
+//   8         loads (TMA): the two tiles of queries, then keys and values in turn through a ring; the next task's while the
+//             last one's outputs are being written
 //   9         issues every tcgen05.mma: S of one tile while the other tile's weights are being computed
 //   10, 11    clean the value tiles that not every row sees whole: rows behind the last key become zero (they are
 //             another sequence's), infinities and NaN too (a weight of zero times one of them would be NaN); the
-//             latter are added back at the end to the rows that do see them
+//             latter are added back at the end to the rows that do see them; warp 10 also hands out the tasks
 // Bound: per pair of tiles of 128 keys (d = 128) the products take 2048 cycles of the tensor pipe, the 32768
 // exponentials as many of the MUFU pipe; so a share of them is computed by a polynomial on the FMA pipe (kPolyOf8).
 // The maximum that weights refer to is raised only when a row exceeds it by 2^8, which spares nearly every rescaling of
@@ -29,16 +30,28 @@ constexpr int kTile = 128, kThreads = 384, kLoader = 8, kIssuer = 9, kGuards = 6
 constexpr int kMost = 96;                                  // weights of a tile that the product starts with
 constexpr int kReady = 8;                                  // value tiles that the guards can be ahead by, at least
 constexpr float kRaise = 8.f;
+constexpr int kSplitBelow = 148, kSplitKeys = 2048, kLeastTiles = 4;   // when pieces are split, and into parts of what size at least
 constexpr int kFewRegs = 80, kManyRegs = 208;              // per thread of warps 8-11, of warps 0-7
 template <int D> __host__ __device__ constexpr int ring_slots() { return D == 128 ? 5 : 10; }
 template <int D> __host__ __device__ constexpr int tile_bytes() { return kTile * D * 2; }
 template <int D> __host__ __device__ constexpr size_t prompt_smem() { return 1024 + (size_t)(2 + ring_slots<D>()) * tile_bytes<D>(); }
 
-struct Shared {
-  uint64_t q_full, full[10], empty[10], raw[kReady], cleaned[kReady], s_full[2], p_most[2], p_ready[2], done[2], drained;
+// What a CTA works on next: a pair of tiles of rows, and of which tiles of keys.
+struct Task {
   Piece piece;
+  int32_t hk, from, to;          // key head; tiles of keys from .. to - 1
+  int32_t slot;                  // where a part of a piece leaves its partial result, or -1: the rows' outputs
+  int32_t index;                 // number of the piece, or -1: there is nothing more to do
+};
+constexpr int kTasks = 4;        // handed out ahead: a task's loads and first products do not wait for the end of the one before
+constexpr int kMostSplit = 160;  // pieces of a call whose pieces are split
+struct Shared {
+  uint64_t q_full, q_free, full[10], empty[10], raw[kReady], cleaned[kReady], s_full[2], p_most[2], p_ready[2], done[2], o_free[2];
+  uint64_t task_full[kTasks], task_free[kTasks], drained;
+  Task task[kTasks];
   uint32_t tmem;
-  int found, abort_flag, wide;
+  int abort_flag, wide[kTasks];
+  int32_t before[kMostSplit + 1];   // tiles of keys of the pieces before each (split calls)
 };
 
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
@@ -63,16 +76,6 @@ __device__ __forceinline__ void tmem_wait(uint32_t (&r)[32]) {
   for (int i = 0; i < 32; i += 8)
     asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]),
                       "+r"(r[i + 7])::"memory");
-}
-__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, "
-      "%25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]),
-      "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]),
-      "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
-      "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(at)
-      : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) {
   asm volatile(
@@ -178,10 +181,58 @@ __device__ __forceinline__ Rows rows_of(const Piece& p, int tile, int per, int c
   return r;
 }
 
+// ---- which CTA does what
+// Many pieces: CTA c of n takes the pieces' (key head fastest) numbers c, 2 n - 1 - c, 2 n + c, ...: of one causal sequence the
+// sizes fall with the number, and going back and forth evens them out.
+// Few pieces (`run` > 0): all tiles of keys of all pieces and key heads, in that order, are dealt out in runs of `run`; a CTA
+// finishes what lies inside its run and leaves partial results of the at most two pieces that do not, its first in slot
+// 2 c, its last in slot 2 c + 1; prompt_join_kernel adds them in the order of the CTAs.
+__device__ __forceinline__ int tiles_of(const Piece& p, int per, int causal) {
+  const Rows a = rows_of(p, 0, per, causal), b = rows_of(p, 1, per, causal);
+  return max(a.tiles, b.tiles);
+}
+// The piece number `index` found by one lane alone (find_piece takes a warp).
+__device__ __forceinline__ bool piece_by_lane(const PromptArgs& a, int rows, int index, Piece& out) {
+  for (int s = a.S - 1; s >= 0; --s) {
+    Piece p;
+    if (!sequence(a, s, p)) report(a.status, DEV_BAD_INDEX);
+    const int n = (p.nq + rows - 1) / rows;
+    if (index < n) {
+      out = p;
+      out.first = (n - 1 - index) * rows;
+      return true;
+    }
+    index -= n;
+  }
+  return false;
+}
+// before[k]: tiles of the pieces 0 .. k - 1, by one warp; returns the sum over all `pieces`.
+__device__ __forceinline__ int sum_tiles(const PromptArgs& a, int per, int pieces, int32_t* before) {
+  const int lane = threadIdx.x & 31;
+  int sum = 0;
+  for (int k0 = 0; k0 < pieces; k0 += 32) {
+    Piece p;
+    const int k = k0 + lane;
+    const int n = k < pieces && piece_by_lane(a, 2 * per, k, p) ? tiles_of(p, per, a.causal) : 0;
+    int x = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += up;
+    }
+    if (k < pieces) before[k] = sum + x - n;
+    sum += __shfl_sync(0xffffffffu, x, 31);
+  }
+  if (lane == 0) before[pieces] = sum;
+  __syncwarp();
+  return sum;
+}
+__host__ __device__ constexpr int64_t part_floats(int d) { return (int64_t)2 * kTile * (d + 2); }
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                 const __grid_constant__ CUtensorMap tmV, const PromptArgs a) {
+                 const __grid_constant__ CUtensorMap tmV, const PromptArgs a, int pieces, int least, float* parts) {
   constexpr int kSlots = ring_slots<D>(), kSub = D / 64, kSubBytes = kTile * 128;
   constexpr uint32_t kColO = 256;
   extern __shared__ uint8_t raw[];
@@ -190,28 +241,23 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   uint8_t* ring = smem + 2 * tile_bytes<D>();
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int G = a.H / a.Hk, per = kTile / G, used = per * G;
-  const int hk = blockIdx.x % a.Hk;
-  if (warp == 0) {
-    Piece p;
-    const bool ok = find_piece(a, 2 * per, blockIdx.x / a.Hk, p);
-    if (lane == 0) { sh.found = ok; sh.piece = p; }
+  if (warp == kIssuer) {
+    tmem_alloc(&sh.tmem, 512);
+    tmem_relinquish();
   } else if (warp == kLoader && lane == 0) {
     prefetch_tmap(&tmQ); prefetch_tmap(&tmK); prefetch_tmap(&tmV);
     mbar_init(&sh.q_full, 1);
+    mbar_init(&sh.q_free, 1);
     for (int i = 0; i < kSlots; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
     for (int i = 0; i < kReady; ++i) { mbar_init(&sh.raw[i], 1); mbar_init(&sh.cleaned[i], kGuards); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_most[i], kTile); mbar_init(&sh.p_ready[i], kTile); mbar_init(&sh.done[i], 1); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_most[i], kTile); mbar_init(&sh.p_ready[i], kTile);
+      mbar_init(&sh.done[i], 1); mbar_init(&sh.o_free[i], kTile);
+    }
+    for (int i = 0; i < kTasks; ++i) { mbar_init(&sh.task_full[i], 1); mbar_init(&sh.task_free[i], kThreads / 32 - 1); }
     mbar_init(&sh.drained, 1);
     sh.abort_flag = 0;
-    sh.wide = 0;
     mbar_fence_init();
-  }
-  __syncthreads();
-  if (!sh.found) return;
-  const Piece pc = sh.piece;
-  if (warp == kIssuer) {                                   // (only CTAs with work hold tensor memory)
-    tmem_alloc(&sh.tmem, 512);
-    tmem_relinquish();
   }
   // rows of a tile that hold no query: whatever was in shared memory might be NaN and slow the softmax down
   for (int i = threadIdx.x; i < 2 * kSub * (kTile - used) * 8; i += kThreads) {
@@ -226,45 +272,74 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   volatile int* abort_flag = &sh.abort_flag;
   auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, a.status, DEV_TIMEOUT_ATTEND); };
   auto wait_warp = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
-  const Rows row0 = rows_of(pc, 0, per, a.causal), row1 = rows_of(pc, 1, per, a.causal);
-  const int tiles = max(row0.tiles, row1.tiles);
-  const int guarded = row0.all / kTile;                    // from here on, not every row sees a whole tile of keys
-
-  // Where an entry of the ring (K 0, V 0, K 1, V 1, ...) lands: its slot's barrier, or for value tiles that the guards have
-  // first a barrier of theirs (they look at no other turn of a slot, and a barrier's phases must not be missed).
-  auto turn_of = [&](int e) { return (e & 1) && (e >> 1) >= guarded ? ((e >> 1) - guarded) / kReady : e / kSlots; };
-  auto landing = [&](int e) { return (e & 1) && (e >> 1) >= guarded ? &sh.raw[((e >> 1) - guarded) % kReady] : &sh.full[e % kSlots]; };
+  // The task number t, for all roles but the one that hands them out; false: no more (or the CTA gave up).
+  auto next_task = [&](int t, Task& task) {
+    if (!wait_warp(&sh.task_full[t % kTasks], (t / kTasks) & 1)) { task.index = -1; return false; }
+    task = sh.task[t % kTasks];
+    return task.index >= 0;
+  };
+  auto end_task = [&](int t) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sh.task_free[t % kTasks]);
+  };
+  // Tiles of keys of a task that a tile of rows takes, and the first of them (absolute) that not every row sees whole.
+  auto share = [&](const Task& k, const Rows& r) { return max(0, min(k.to, r.tiles) - k.from); };
 
   // The softmax needs the registers: a row of logits is 128 of them.  (What the block was launched with covers the shares:
   // the host checks it.)  Each warp of a group of four moves its share in its own branch.
   if (warp >= kLoader) {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
+
   if (warp == kLoader) {
-    int e = 0;
+    int e = 0, g = 0, t = 0;                               // entries of the ring, value tiles that the guards have first, tasks
     bool ok = true;
-    if (elect_one() && tiles > 0) {
-      mbar_expect_tx(&sh.q_full, (row1.tiles ? 2 : 1) * kSub * used * 128);
-      for (int i = 0; i < (row1.tiles ? 2 : 1); ++i)
-        for (int s = 0; s < kSub; ++s)
-          tma_load_3d(smem + (i * kSub + s) * kSubBytes, &tmQ, 64 * s, hk * G, pc.q0 + pc.first + i * per, &sh.q_full);
-    }
-    __syncwarp();
-    for (; e < 2 * tiles; ++e) {
-      const int slot = e % kSlots;
-      if (e >= kSlots && !(ok = wait_warp(&sh.empty[slot], ((e / kSlots) - 1) & 1))) break;
-      if (elect_one()) {
-        uint64_t* bar = landing(e);
-        if (bar != &sh.full[slot]) mbar_arrive(&sh.full[slot]);   // (nobody waits for this turn of the slot: it only passes)
-        mbar_expect_tx(bar, tile_bytes<D>());
-        for (int s = 0; s < kSub; ++s)
-          tma_load_3d(ring + slot * tile_bytes<D>() + s * kSubBytes, (e & 1) ? &tmV : &tmK, 64 * s, hk, pc.k0 + (e >> 1) * kTile, bar);
+    uint32_t last = 0;                                     // (giving up: whether the last entries landed at their slot's barrier)
+    Task task;
+    for (; ok && next_task(t, task); ++t) {
+      const Rows row0 = rows_of(task.piece, 0, per, a.causal), row1 = rows_of(task.piece, 1, per, a.causal);
+      const int guarded = row0.all / kTile, both = share(task, row1) > 0 ? 2 : 1;
+      // (every task is one turn of q_full and of q_free, also one without keys: no turn may be missed)
+      if (t > 0 && !(ok = wait_warp(&sh.q_free, (t - 1) & 1))) break;
+      if (task.to > task.from) {
+        if (elect_one()) {
+          // (a tile that takes no part is not loaded; whichever of the two it is, the other's place stays its own)
+          const int lo = share(task, row0) > 0 ? 0 : 1;
+          mbar_expect_tx(&sh.q_full, (both - lo) * kSub * used * 128);
+          for (int i = lo; i < both; ++i)
+            for (int s = 0; s < kSub; ++s)
+              tma_load_3d(smem + (i * kSub + s) * kSubBytes, &tmQ, 64 * s, task.hk * G, task.piece.q0 + task.piece.first + i * per, &sh.q_full);
+        }
+        __syncwarp();
+      } else if (lane == 0) {
+        mbar_arrive(&sh.q_full);
       }
-      __syncwarp();
+      for (int x = 2 * task.from; x < 2 * task.to; ++x, ++e) {
+        const int slot = e % kSlots, j = x >> 1;
+        if (e >= kSlots && !(ok = wait_warp(&sh.empty[slot], ((e / kSlots) - 1) & 1))) break;
+        // Value tiles that the guards have first land at a barrier of theirs (they look at no other turn of a slot, and a
+        // barrier's phases must not be missed); the slot's own barrier only passes.
+        const bool guard = (x & 1) && j >= guarded;
+        if (elect_one()) {
+          uint64_t* bar = guard ? &sh.raw[g % kReady] : &sh.full[slot];
+          if (guard) mbar_arrive(&sh.full[slot]);
+          mbar_expect_tx(bar, tile_bytes<D>());
+          for (int s = 0; s < kSub; ++s)
+            tma_load_3d(ring + slot * tile_bytes<D>() + s * kSubBytes, (x & 1) ? &tmV : &tmK, 64 * s, task.hk, task.piece.k0 + j * kTile, bar);
+        }
+        __syncwarp();
+        last = last << 1 | (guard ? 1u : 0u);
+        g += guard;
+      }
+      end_task(t);
     }
-    if (!ok) {                                             // no copy is left in flight when the CTA ends
+    if (!ok || *abort_flag) {                              // no copy is left in flight when the CTA ends
       int none = 0;
-      mbar_wait(&sh.q_full, 0, &none, a.status, DEV_TIMEOUT_ATTEND);
-      for (int i = max(0, e - kSlots); i < e; ++i) mbar_wait(landing(i), turn_of(i) & 1, &none, a.status, DEV_TIMEOUT_ATTEND);
+      if (t > 0 || e > 0) mbar_wait(&sh.q_full, t & 1, &none, a.status, DEV_TIMEOUT_ATTEND);
+      for (int i = 0; i < min(e, kSlots); ++i) {
+        const int x = e - 1 - i;
+        if (last >> i & 1) { --g; mbar_wait(&sh.raw[g % kReady], (g / kReady) & 1, &none, a.status, DEV_TIMEOUT_ATTEND); }
+        else mbar_wait(&sh.full[x % kSlots], (x / kSlots) & 1, &none, a.status, DEV_TIMEOUT_ATTEND);
+      }
     }
   } else if (warp == kIssuer) {
     const uint32_t q_at = smem_u32(smem), r_at = smem_u32(ring);
@@ -285,194 +360,356 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                      umma_desc_sw128_mn(r_at + slot * tile_bytes<D>() + k * 2048, kSubBytes), kIdO, more || k > 0);
     };
     auto full = [&](int e) { return wait_warp(&sh.full[e % kSlots], (e / kSlots) & 1); };
-    bool ok = tiles == 0 || (wait_warp(&sh.q_full, 0) && full(0));
-    tc_fence_after();
-    if (ok && tiles > 0) {
-      if (elect_one()) {
-        if (row0.tiles > 0) issue_s(0, 0);
-        if (row1.tiles > 0) issue_s(1, 0);
-        umma_commit(&sh.empty[0]);
-      }
-      __syncwarp();
-    }
-    for (int j = 0; ok && j < tiles; ++j) {
-      const int ev = 2 * j + 1, ek = 2 * j + 2;
-      ok = j < guarded ? full(ev) : wait_warp(&sh.cleaned[(j - guarded) % kReady], ((j - guarded) / kReady) & 1);
-      if (ok && j + 1 < tiles) ok = full(ek);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int n = i ? row1.tiles : row0.tiles;
-        if (j < n) {
-          ok = ok && wait_warp(&sh.p_most[i], j & 1);
-          if (!ok) break;
-          tc_fence_after();
-          if (elect_one()) issue_o(i, ev % kSlots, 0, kMost / 16, j > 0);
-          __syncwarp();
-          if (!(ok = wait_warp(&sh.p_ready[i], j & 1))) break;
-          tc_fence_after();
-          if (elect_one()) {
-            issue_o(i, ev % kSlots, kMost / 16, kTile / 16, true);
-            if (j + 1 < n) issue_s(i, ek % kSlots);
-            else umma_commit(&sh.done[i]);
-          }
-          __syncwarp();
+    bool ok = true;
+    int e0 = 0, g = 0;                                     // entries and guarded value tiles of the tasks before
+    int turn[2] = {0, 0}, took[2] = {0, 0};                // tiles of keys, tasks that each tile of rows has taken
+    Task task;
+    for (int t = 0; ok && next_task(t, task); ++t) {
+      const Rows row0 = rows_of(task.piece, 0, per, a.causal), row1 = rows_of(task.piece, 1, per, a.causal);
+      const int guarded = row0.all / kTile, tiles = task.to - task.from;
+      const int n[2] = {share(task, row0), share(task, row1)};
+      if (!(ok = wait_warp(&sh.q_full, t & 1))) break;
+      if (tiles > 0) {
+        if (!(ok = full(e0))) break;
+        tc_fence_after();
+        if (elect_one()) {
+          if (n[0] > 0) issue_s(0, e0 % kSlots);
+          if (n[1] > 0) issue_s(1, e0 % kSlots);
+          umma_commit(&sh.empty[e0 % kSlots]);
+          if (tiles == 1) umma_commit(&sh.q_free);
         }
+        __syncwarp();
       }
-      if (ok && elect_one()) {
-        umma_commit(&sh.empty[ev % kSlots]);
-        if (j + 1 < tiles) umma_commit(&sh.empty[ek % kSlots]);
+      for (int j = 0; ok && j < tiles; ++j) {
+        const int ev = e0 + 2 * j + 1, ek = ev + 1;
+        if (task.from + j < guarded) ok = full(ev);
+        else { ok = wait_warp(&sh.cleaned[g % kReady], (g / kReady) & 1); ++g; }
+        if (ok && j + 1 < tiles) ok = full(ek);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (j < n[i]) {
+            // (the outputs of this tile's last task have been read before they are overwritten)
+            if (j == 0 && took[i] > 0) ok = ok && wait_warp(&sh.o_free[i], (took[i] - 1) & 1);
+            ok = ok && wait_warp(&sh.p_most[i], (turn[i] + j) & 1);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) issue_o(i, ev % kSlots, 0, kMost / 16, j > 0);
+            __syncwarp();
+            if (!(ok = wait_warp(&sh.p_ready[i], (turn[i] + j) & 1))) break;
+            tc_fence_after();
+            if (elect_one()) {
+              issue_o(i, ev % kSlots, kMost / 16, kTile / 16, true);
+              if (j + 1 < n[i]) issue_s(i, ek % kSlots);
+              else umma_commit(&sh.done[i]);
+            }
+            __syncwarp();
+          }
+        }
+        if (ok && elect_one()) {
+          umma_commit(&sh.empty[ev % kSlots]);
+          if (j + 1 < tiles) umma_commit(&sh.empty[ek % kSlots]);
+          if (j + 2 == tiles) umma_commit(&sh.q_free);     // the task's last logits have been issued
+        }
+        __syncwarp();
       }
-      __syncwarp();
+      if (tiles == 0 && lane == 0) mbar_arrive(&sh.q_free);
+      e0 += 2 * tiles;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) { turn[i] += n[i]; took[i] += n[i] > 0; }
+      end_task(t);
     }
-    if (!ok) {                                             // products in flight end before tensor memory is given back
+    if (!ok || *abort_flag) {                              // products in flight end before tensor memory is given back
       if (elect_one()) umma_commit(&sh.drained);
       __syncwarp();
       int none = 0;
       mbar_wait(&sh.drained, 0, &none, a.status, DEV_TIMEOUT_ATTEND);
     }
-  } else if (warp > kIssuer) {
+  } else {
+    // The guards; the first of their warps hands out the tasks too.
+    const bool chief = warp == kIssuer + 1;
     const int id = threadIdx.x - 32 * (kIssuer + 1);
-    bool wide = false;
-    for (int j = guarded; j < tiles; ++j) {
-      const int e = 2 * j + 1, slot = e % kSlots;
-      if (!wait_warp(landing(e), turn_of(e) & 1)) break;
-      const int keys = pc.nk - j * kTile;
-      uint4* v = reinterpret_cast<uint4*>(ring + slot * tile_bytes<D>());
-      for (int i = id; i < tile_bytes<D>() / 16; i += kGuards) {
-        const int r = (i >> 3) & (kTile - 1);
-        if (r >= keys) {
-          v[i] = make_uint4(0, 0, 0, 0);
-          continue;
+    int e0 = 0, g = 0, number = blockIdx.x, round = 0;
+    int64_t at = 0, end = 0;
+    if (chief && least > 0) {
+      const int64_t total = (int64_t)sum_tiles(a, per, pieces, sh.before) * a.Hk, run = run_of(total, gridDim.x, least);
+      at = (int64_t)blockIdx.x * run;
+      end = min(at + run, total);
+    }
+    auto hand_out = [&](int t) {                           // false: the CTA gave up
+      Task task = {};
+      task.index = -1;
+      task.slot = -1;
+      if (least > 0) {
+        if (at < end) {
+          int k = 0;                                       // the last piece that begins at or before `at` and has tiles
+          for (int x = lane; x < pieces; x += 32)
+            if ((int64_t)sh.before[x] * a.Hk <= at && sh.before[x + 1] > sh.before[x]) k = max(k, x);
+          k = __reduce_max_sync(0xffffffffu, k);
+          find_piece(a, 2 * per, k, task.piece);
+          const int U = sh.before[k + 1] - sh.before[k];
+          const int rel = (int)(at - (int64_t)sh.before[k] * a.Hk);
+          task.index = k;
+          task.hk = rel / U;
+          task.from = rel % U;
+          task.to = (int)min((int64_t)U, task.from + (end - at));
+          if (task.from > 0 || task.to < U) task.slot = 2 * blockIdx.x + (task.from == 0);
+          at += task.to - task.from;
         }
-        const uint4 x = v[i];
-        uint32_t w[4] = {x.x, x.y, x.z, x.w};
-        // an exponent of all ones in either half: with the low bits masked off the sum carries out of it
-        uint32_t odd = 0;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) odd |= ((w[q] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-        if (odd) {
-          wide = true;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const uint32_t bits = ((w[q] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-            if (bits & 0x8000u) w[q] &= 0xffff0000u;
-            if (bits & 0x80000000u) w[q] &= 0x0000ffffu;
-          }
-          v[i] = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {
+        if (find_piece(a, 2 * per, number / a.Hk, task.piece)) {
+          task.index = number / a.Hk;
+          task.hk = number % a.Hk;
+          task.to = tiles_of(task.piece, per, a.causal);
         }
+        number = ++round & 1 ? (round + 1) * (int)gridDim.x - 1 - blockIdx.x : round * (int)gridDim.x + blockIdx.x;
       }
-      if (wide) *reinterpret_cast<volatile int*>(&sh.wide) = 1;
-      fence_proxy_async();
-      mbar_arrive(&sh.cleaned[(j - guarded) % kReady]);
+      if (t >= kTasks && !wait_warp(&sh.task_free[t % kTasks], ((t / kTasks) - 1) & 1)) return false;
+      if (lane == 0) {
+        sh.task[t % kTasks] = task;
+        sh.wide[t % kTasks] = 0;
+        mbar_arrive(&sh.task_full[t % kTasks]);
+      }
+      __syncwarp();
+      return true;
+    };
+    bool ok = !chief || hand_out(0);
+    Task task;
+    for (int t = 0; ok && next_task(t, task); ++t) {
+      if (chief) ok = hand_out(t + 1);
+      const int guarded = rows_of(task.piece, 0, per, a.causal).all / kTile;
+      bool wide = false;
+      for (int j = max(guarded, task.from); ok && j < task.to; ++j, ++g) {
+        const int slot = (e0 + 2 * (j - task.from) + 1) % kSlots;
+        if (!(ok = wait_warp(&sh.raw[g % kReady], (g / kReady) & 1))) break;
+        const int keys = task.piece.nk - j * kTile;
+        uint4* v = reinterpret_cast<uint4*>(ring + slot * tile_bytes<D>());
+        for (int i = id; i < tile_bytes<D>() / 16; i += kGuards) {
+          const int r = (i >> 3) & (kTile - 1);
+          if (r >= keys) {
+            v[i] = make_uint4(0, 0, 0, 0);
+            continue;
+          }
+          const uint4 x = v[i];
+          uint32_t w[4] = {x.x, x.y, x.z, x.w};
+          // an exponent of all ones in either half: with the low bits masked off the sum carries out of it
+          uint32_t odd = 0;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) odd |= ((w[q] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+          if (odd) {
+            wide = true;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const uint32_t bits = ((w[q] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+              if (bits & 0x8000u) w[q] &= 0xffff0000u;
+              if (bits & 0x80000000u) w[q] &= 0x0000ffffu;
+            }
+            v[i] = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+        if (wide) *reinterpret_cast<volatile int*>(&sh.wide[t % kTasks]) = 1;
+        fence_proxy_async();
+        mbar_arrive(&sh.cleaned[g % kReady]);
+      }
+      e0 += 2 * (task.to - task.from);
+      if (!chief) end_task(t);
     }
   }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegs));
     const int i = warp >> 2, r = threadIdx.x & 127;
-    const Rows rows = i ? row1 : row0;
     const uint32_t at = tmem + ((uint32_t)(32 * (warp & 3)) << 16), at_s = at + 128 * i, at_o = at + kColO + 128 * i;
-    const int token = rows.first + r / G;                  // within the sequence
-    const int sees = a.causal ? max(0, min(pc.nk, token + 1 + pc.nk - pc.nq)) : pc.nk;
     const float c = a.scale * kLog2e;
-    float m = -INFINITY, l = 0.f;
     bool ok = true;
-    for (int j = 0; j < rows.tiles; ++j) {
-      if (!(ok = wait_warp(&sh.s_full[i], j & 1))) break;
-      tc_fence_after();
-      uint32_t s[4][32];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) tmem_ld32(at_s + 32 * q, s[q]);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) tmem_wait(s[q]);
-      const bool edge = (j + 1) * kTile > rows.all;
-      if (edge) {
-        const int n = sees - j * kTile;
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-          for (int k = 0; k < 32; ++k)
-            if (32 * q + k >= n) s[q][k] = 0xff800000u;
+    int turn = 0, took = 0, guards = 0;                    // tiles of keys and tasks of this tile of rows, guarded value tiles
+    for (int t = 0; ok; ++t) {
+      // (the task's fields are read where they are needed: the registers are the logits')
+      const volatile Task& task = sh.task[t % kTasks];
+      if (!wait_warp(&sh.task_full[t % kTasks], (t / kTasks) & 1) || task.index < 0) break;
+      int n, from, all, sees;
+      {
+        const Piece pc = {task.piece.q0, task.piece.nq, task.piece.k0, task.piece.nk, task.piece.first};
+        const Rows rows = rows_of(pc, i, per, a.causal);
+        const int token = rows.first + r / G;              // within the sequence
+        from = task.from;
+        n = max(0, min(task.to, rows.tiles) - from);
+        all = rows.all;
+        sees = a.causal ? max(0, min(pc.nk, token + 1 + pc.nk - pc.nq)) : pc.nk;
       }
-      // The weights of all but the last quarter are taken with the maximum of the tiles before; the tile's own is found on
-      // the side.  Only where it is higher by 2^8 (or there is none before, or a NaN) they are taken again.
-      float mx = -INFINITY, sum = 0.f;
-      if (j == 0) mx = row_max(s);
-      else sum = edge ? weights<true, 0, kMost / 32>(s, c, reference(m, c), at_s, &mx) : weights<false, 0, kMost / 32>(s, c, reference(m, c), at_s, &mx);
-      if (__any_sync(0xffffffffu, !((mx - m) * c <= kRaise))) {
-        const float up = max3_nan(m, mx, mx);
-        const float f = up == m || up == -INFINITY ? 1.f : ex2((m - up) * c);
-        m = up;
-        l *= f;
-        if (j > 0) {
-          // S of this tile was issued behind O of the tile before, so O is complete
+      float m = -INFINITY, l = 0.f;
+      for (int jj = 0; jj < n; ++jj) {
+        const int j = from + jj;
+        if (!(ok = wait_warp(&sh.s_full[i], (turn + jj) & 1))) break;
+        tc_fence_after();
+        uint32_t s[4][32];
 #pragma unroll
-          for (int q = 0; q < D / 32; ++q) {
-            uint32_t o[32];
-            tmem_ld32(at_o + 32 * q, o);
-            tmem_wait(o);
+        for (int q = 0; q < 4; ++q) tmem_ld32(at_s + 32 * q, s[q]);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-            tmem_st32(at_o + 32 * q, o);
-          }
+        for (int q = 0; q < 4; ++q) tmem_wait(s[q]);
+        const bool edge = (j + 1) * kTile > all;
+        if (edge) {
+          const int most = sees - j * kTile;
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+              if (32 * q + k >= most) s[q][k] = 0xff800000u;
         }
-        sum = weights<true, 0, kMost / 32>(s, c, reference(m, c), at_s, nullptr);
-      }
-      tmem_st_wait();
-      tc_fence_before();
-      mbar_arrive(&sh.p_most[i]);
-      sum += edge ? weights<true, kMost / 32, 4>(s, c, reference(m, c), at_s, nullptr) : weights<false, kMost / 32, 4>(s, c, reference(m, c), at_s, nullptr);
-      tmem_st_wait();
-      tc_fence_before();
-      mbar_arrive(&sh.p_ready[i]);
-      l += sum;
-    }
-    if (ok && rows.tiles > 0) ok = wait_warp(&sh.done[i], 0);
-    if (ok && rows.tiles > guarded && rows.tiles > 0) {    // (whether a value was set to zero)
-      const int g = tiles - 1 - guarded;
-      ok = g < 0 || wait_warp(&sh.cleaned[g % kReady], (g / kReady) & 1);
-    }
-    tc_fence_after();
-    if (ok) {
-      const bool mine = r < used && token < pc.nq && rows.count > 0;
-      const bool wide = *reinterpret_cast<volatile int*>(&sh.wide) != 0;
-      const int64_t t = (int64_t)pc.q0 + token;
-      const int h = hk * G + r % G;
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      __nv_bfloat16* Y = static_cast<__nv_bfloat16*>(a.Y) + t * a.y_stride + (int64_t)h * D;
+        // The weights of all but the last quarter are taken with the maximum of the tiles before; the tile's own is found on
+        // the side.  Only where it is higher by 2^8 (or there is none before, or a NaN) they are taken again.
+        float mx = -INFINITY, sum = 0.f;
+        if (jj == 0) mx = row_max(s);
+        else sum = edge ? weights<true, 0, kMost / 32>(s, c, reference(m, c), at_s, &mx) : weights<false, 0, kMost / 32>(s, c, reference(m, c), at_s, &mx);
+        if (__any_sync(0xffffffffu, !((mx - m) * c <= kRaise))) {
+          const float up = max3_nan(m, mx, mx);
+          const float f = up == m || up == -INFINITY ? 1.f : ex2((m - up) * c);
+          m = up;
+          l *= f;
+          if (jj > 0) {
+            // S of this tile was issued behind O of the tile before, so O is complete
 #pragma unroll
-      for (int q = 0; q < D / 32; ++q) {
-        uint32_t o[32];
-        if (rows.tiles > 0) {
-          tmem_ld32(at_o + 32 * q, o);
-          tmem_wait(o);
-        }
-        float y[32];
+            for (int q = 0; q < D / 16; ++q) {
+              float o[16];
+              uint32_t w[16];
+              tmem_ld16(at_o + 16 * q, o);
 #pragma unroll
-        for (int k = 0; k < 32; ++k) y[k] = l == 0.f ? 0.f : __uint_as_float(o[k]) * inv;
-        if (wide && mine) {                                // rare: infinities and NaN of the cleaned tiles, where seen
-          for (int k = guarded * kTile; k < sees; ++k) {
-            const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.V) + (int64_t)(pc.k0 + k) * a.v_stride + (int64_t)hk * D + 32 * q;
-#pragma unroll
-            for (int x = 0; x < 32; ++x) {
-              const float f = __bfloat162float(v[x]);
-              if (!isfinite(f)) y[x] += f;
+              for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(o[k] * f);
+              tmem_st16(at_o + 16 * q, w);
             }
           }
+          sum = weights<true, 0, kMost / 32>(s, c, reference(m, c), at_s, nullptr);
         }
-        if (mine) {
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(&sh.p_most[i]);
+        sum += edge ? weights<true, kMost / 32, 4>(s, c, reference(m, c), at_s, nullptr) : weights<false, kMost / 32, 4>(s, c, reference(m, c), at_s, nullptr);
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(&sh.p_ready[i]);
+        l += sum;
+      }
+      turn += n;
+      const Piece pc = {task.piece.q0, task.piece.nq, task.piece.k0, task.piece.nk, task.piece.first};
+      const int first = max(rows_of(pc, 0, per, a.causal).all / kTile, from);   // of the value tiles of this task that the guards had
+      const int cleaned = max(0, task.to - first), token = pc.first + i * per + r / G;
+      if (ok && n > 0) ok = wait_warp(&sh.done[i], took & 1);
+      // (whether a value was set to zero: the last of the task's cleaned tiles tells for all, and the product with it is over)
+      if (ok && cleaned > 0) ok = wait_warp(&sh.cleaned[(guards + cleaned - 1) % kReady], ((guards + cleaned - 1) / kReady) & 1);
+      guards += cleaned;
+      took += n > 0;
+      tc_fence_after();
+      if (ok) {
+        const bool mine = r < used && token < pc.nq;
+        const int slot = task.slot, hk = task.hk, to = task.to;
+        const bool wide = *reinterpret_cast<volatile int*>(&sh.wide[t % kTasks]) != 0;
+        const int64_t row = (int64_t)pc.q0 + token;
+        const int h = hk * G + r % G;
+        const float inv = slot >= 0 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+        __nv_bfloat16* Y = static_cast<__nv_bfloat16*>(a.Y) + row * a.y_stride + (int64_t)h * D;
+        float* part = parts + (int64_t)max(slot, 0) * part_floats(D) + (i * kTile + r) * D;
 #pragma unroll
-          for (int k = 0; k < 32; k += 8)
-            *reinterpret_cast<uint4*>(Y + 32 * q + k) = make_uint4(pack_bf16(y[k], y[k + 1]), pack_bf16(y[k + 2], y[k + 3]),
-                                                                   pack_bf16(y[k + 4], y[k + 5]), pack_bf16(y[k + 6], y[k + 7]));
+        for (int q = 0; q < D / 32; ++q) {
+          uint32_t o[32];
+          if (n > 0) {
+            tmem_ld32(at_o + 32 * q, o);
+            tmem_wait(o);
+          }
+          if (q == D / 32 - 1 && n > 0) {                  // the next task may have the outputs' place
+            tc_fence_before();
+            mbar_arrive(&sh.o_free[i]);
+          }
+          float y[32];
+#pragma unroll
+          for (int k = 0; k < 32; ++k) y[k] = l == 0.f ? 0.f : __uint_as_float(o[k]) * inv;
+          if (wide && mine) {                              // rare: infinities and NaN of the cleaned tiles, where seen
+            for (int k = first * kTile; k < min(sees, to * kTile); ++k) {
+              const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.V) + (int64_t)(pc.k0 + k) * a.v_stride + (int64_t)hk * D + 32 * q;
+#pragma unroll
+              for (int x = 0; x < 32; ++x) {
+                const float f = __bfloat162float(v[x]);
+                if (!isfinite(f)) y[x] += f;
+              }
+            }
+          }
+          if (slot >= 0) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(part + 32 * q + k) = make_float4(y[k], y[k + 1], y[k + 2], y[k + 3]);
+          } else if (mine) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 8)
+              *reinterpret_cast<uint4*>(Y + 32 * q + k) = make_uint4(pack_bf16(y[k], y[k + 1]), pack_bf16(y[k + 2], y[k + 3]),
+                                                                     pack_bf16(y[k + 4], y[k + 5]), pack_bf16(y[k + 6], y[k + 7]));
+          }
+        }
+        if (slot >= 0) {
+          float* stat = parts + (int64_t)slot * part_floats(D) + 2 * kTile * D + i * kTile + r;
+          stat[0] = m == -INFINITY ? -INFINITY : m * c;
+          stat[2 * kTile] = l;
+        } else if (mine && a.lse) {
+          a.lse[row * a.H + h] = l == 0.f ? -INFINITY : (m * c + log2f(l)) * kLn2;
         }
       }
-      if (mine && a.lse) a.lse[t * a.H + h] = l == 0.f ? -INFINITY : (m * c + log2f(l)) * kLn2;
+      end_task(t);
     }
     tc_fence_before();
   }
   __syncthreads();
   tc_fence_after();
   if (warp == kIssuer) tmem_dealloc(tmem, 512);
+}
+
+// ---- partial results of split pieces.  A warp per row, 32 rows to a CTA: nothing to do if one CTA had the whole piece, zeros
+// if its rows see no key; else the parts are brought to their common maximum and added in the order of the CTAs.
+constexpr int kJoinRows = 32, kJoinThreads = 256;
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads) prompt_join_kernel(const PromptArgs a, int pieces, int least, int ctas, const float* parts) {
+  __shared__ int32_t before[kMostSplit + 1];
+  __shared__ Piece shared_piece;
+  __shared__ int found;
+  const int G = a.H / a.Hk, per = kTile / G, k = blockIdx.x / a.Hk, hk = blockIdx.x % a.Hk;
+  if (threadIdx.x < 32) {
+    sum_tiles(a, per, pieces, before);
+    Piece p;
+    const bool ok = find_piece(a, 2 * per, k, p);
+    if (threadIdx.x == 0) { found = ok; shared_piece = p; }
+  }
+  __syncthreads();
+  if (!found) return;
+  const Piece pc = shared_piece;
+  const int U = before[k + 1] - before[k];
+  const int64_t run = run_of((int64_t)before[pieces] * a.Hk, ctas, least), g0 = (int64_t)before[k] * a.Hk + (int64_t)hk * U;
+  const int c0 = (int)(g0 / run), c1 = U > 0 ? (int)((g0 + U - 1) / run) : c0;
+  if (U > 0 && c0 == c1) return;
+  pdl_wait();                                              // the parts come from the kernel before
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int kPer = D / 32;
+  for (int r = blockIdx.y * kJoinRows + warp; r < (int)(blockIdx.y + 1) * kJoinRows; r += kJoinThreads / 32) {
+    const int i = r / kTile, x = r % kTile, token = pc.first + i * per + x / G;
+    if (x >= per * G || token >= pc.nq) continue;
+    float m = -INFINITY, l = 0.f, y[kPer] = {};
+    auto slot = [&](int n) { return parts + (int64_t)(2 * (c0 + n) + (n == 0)) * part_floats(D); };
+    const int n = U > 0 ? c1 - c0 + 1 : 0;
+    for (int p = 0; p < n; ++p) m = fmaxf(m, ld_after_wait(slot(p) + 2 * kTile * D + r));
+    const float use = m == -INFINITY ? 0.f : m;
+    for (int p = 0; p < n; ++p) {
+      const float* s = slot(p);
+      const float top = ld_after_wait(s + 2 * kTile * D + r), sum = ld_after_wait(s + 2 * kTile * D + 2 * kTile + r);
+      float v[kPer];
+#pragma unroll
+      for (int q = 0; q < kPer; ++q) v[q] = ld_after_wait(s + r * D + lane + 32 * q);
+      const float w = exp2f(top - use);
+      if (w == 0.f) continue;
+      l = fmaf(w, sum, l);
+#pragma unroll
+      for (int q = 0; q < kPer; ++q) y[q] = fmaf(w, v[q], y[q]);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int64_t row = (int64_t)pc.q0 + token;
+    const int h = hk * G + x % G;
+    __nv_bfloat16* Y = static_cast<__nv_bfloat16*>(a.Y) + row * a.y_stride + (int64_t)h * D;
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) Y[lane + 32 * q] = __float2bfloat16_rn(y[q] * inv);
+    if (a.lse && lane == 0) a.lse[row * a.H + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  }
 }
 
 // Whether the block's registers at launch cover the shares that its warps ask for (or they would wait for good).
@@ -504,14 +741,24 @@ avq_status launch(const PromptArgs& a, cudaStream_t st) {
   s = open_shared_memory<prompt_tc_kernel<D>>(dev);
   if (s != AVQ_OK) return s;
   if (!registers_cover<D>()) return AVQ_ERR_CUDA;
-  const int64_t grid = most_pieces(a.Tq, a.S, 2 * per) * a.Hk;
-  if (grid >= (int64_t)1 << 31) return AVQ_ERR_UNSUPPORTED;
-  prompt_tc_kernel<D><<<(unsigned)grid, kThreads, prompt_smem<D>(), st>>>(tmQ, tmK, tmV, a);
-  return cuda_ok(cudaGetLastError());
+  int sms = 0;
+  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return AVQ_ERR_CUDA;
+  sms = sms < kPromptCtas ? sms : kPromptCtas;
+  const int64_t pieces = most_pieces(a.Tq, a.S, 2 * per), all = pieces * a.Hk;
+  if (all >= (int64_t)1 << 30) return AVQ_ERR_UNSUPPORTED;
+  // Pieces that cannot fill the GPU, over keys that can be long, are split, if the caller's workspace holds the parts.
+  const bool split = a.parts && all <= kSplitBelow && pieces <= kMostSplit && a.Tk >= kSplitKeys;
+  const int grid = split ? sms : (int)(all < sms ? all : sms), least = split ? kLeastTiles : 0;
+  prompt_tc_kernel<D><<<grid, kThreads, prompt_smem<D>(), st>>>(tmQ, tmK, tmV, a, (int)pieces, least, a.parts);
+  if (cudaGetLastError() != cudaSuccess) return AVQ_ERR_CUDA;
+  if (!split) return AVQ_OK;
+  return cuda_ok(launch_pdl(prompt_join_kernel<D>, dim3((unsigned)all, 2 * kTile / kJoinRows), dim3(kJoinThreads), 0, st, true, a, (int)pieces,
+                            least, grid, (const float*)a.parts));
 }
 
 }  // namespace
 
+size_t tc_prompt_part_bytes(int d) { return sizeof(float) * 2 * kPromptCtas * (size_t)part_floats(d); }
 avq_status tc_prompt(const PromptArgs& a, cudaStream_t st) { return a.d == 64 ? launch<64>(a, st) : launch<128>(a, st); }
 
 }  // namespace exact
