@@ -13,8 +13,10 @@
 //   10, 11    clean the value tiles that not every row sees whole: rows behind the last key become zero (they are
 //             another sequence's), infinities and NaN too (a weight of zero times one of them would be NaN); the
 //             latter are added back at the end to the rows that do see them; warp 10 also hands out the tasks
-// Bound: per pair of tiles of 128 keys (d = 128) the products take 2048 cycles of the tensor pipe, the 32768
-// exponentials as many of the MUFU pipe; so a share of them is computed by a polynomial on the FMA pipe (kPolyOf8).
+// Bound: per pair of tiles of 128 keys (d = 128) the products take 2048 cycles of the tensor pipe and the 32768
+// exponentials as many of the MUFU pipe, in turn for each tile of rows; what keeps them from overlapping fully is the way
+// from logits to weights and back.  A quarter of the exponentials by a polynomial on the FMA pipe was 4 % slower than
+// none (16384 tokens of 16 heads: 949 and 906 us): a second form of the code costs more than the pipe gains.
 // The maximum that weights refer to is raised only when a row exceeds it by 2^8, which spares nearly every rescaling of
 // O: weights stay below 2^8, and what they are relative to cancels in O / l.
 #include "avq_exact.cuh"
@@ -51,7 +53,7 @@ struct Shared {
   Task task[kTasks];
   uint32_t tmem;
   int abort_flag, wide[kTasks];
-  int32_t before[kMostSplit + 1];   // tiles of keys of the pieces before each (split calls)
+  int32_t before[kMostSplit + 1];   // split calls: tiles of keys of the pieces before each
 };
 
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
@@ -85,6 +87,10 @@ __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) 
       "r"(r[14]), "r"(r[15]), "r"(at)
       : "memory");
 }
+__device__ __forceinline__ void store32(void* to, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e, uint32_t f, uint32_t g, uint32_t h) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h)
+               : "memory");
+}
 __device__ __forceinline__ float ex2(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -96,26 +102,6 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// 2^x of two values up to 2^8 on the FMA pipe: the nearest integer n by adding 1.5 * 2^23, 2^(x - n) on [-1/2, 1/2] by a
-// polynomial of degree 3 fitted for the smallest largest relative error (7.5e-5; the weights are rounded to bfloat16,
-// 3.9e-3, next), n added to the exponent.  Below -126: 2^-126.  A NaN gives anything: its row's maximum is NaN too.
-__device__ __forceinline__ void poly_ex2(f32x2 x, float& lo, float& hi) {
-  float a, b;
-  unpack2(x, a, b);
-  x = pack2(fmaxf(a, -126.f), fmaxf(b, -126.f));
-  const f32x2 magic = pack2(12582912.f, 12582912.f), minus = pack2(-12582912.f, -12582912.f), neg = pack2(-1.f, -1.f);
-  const f32x2 n = add2(x, magic), f = fma2(add2(n, minus), neg, x);
-  f32x2 y = fma2(f, pack2(0.0551716685f, 0.0551716685f), pack2(0.242611125f, 0.242611125f));
-  y = fma2(y, f, pack2(0.693260968f, 0.693260968f));
-  y = fma2(y, f, pack2(0.999928057f, 0.999928057f));
-  float n0, n1, y0, y1;
-  unpack2(n, n0, n1);
-  unpack2(y, y0, y1);
-  lo = __uint_as_float(__float_as_uint(y0) + (__float_as_uint(n0) << 23));
-  hi = __uint_as_float(__float_as_uint(y1) + (__float_as_uint(n1) << 23));
-}
-constexpr int kPolyOf8 = 2;                                // pairs of 8 whose exponentials the polynomial computes
-
 // What is added to scale * logit, in powers of two: an infinite or NaN maximum makes every weight of the row NaN.
 __device__ __forceinline__ float reference(float m, float c) {
   return m == -INFINITY ? 0.f : isfinite(m) ? -m * c : __int_as_float(0x7fffffff);
@@ -132,9 +118,8 @@ __device__ __forceinline__ float row_max(const uint32_t (&s)[4][32]) {
   return max3_nan(max3_nan(top[0], top[1], top[2]), top[3], top[3]);
 }
 // Weights of the 32-column quarters FROM .. TO - 1 of a row, as bfloat16 over the row's logits in tensor memory; returns
-// their sum.  EDGE: the tile holds masked logits, whose weights have to be exactly zero (no polynomial).  mx: gets the
-// maximum of the whole row.
-template <bool EDGE, int FROM, int TO>
+// their sum.  mx: gets the maximum of the whole row.
+template <int FROM, int TO>
 __device__ __forceinline__ float weights(const uint32_t (&s)[4][32], float c, float sub, uint32_t at, float* mx) {
   const f32x2 c2 = pack2(c, c), sub2 = pack2(sub, sub);
   f32x2 sum[2] = {0ull, 0ull};
@@ -146,13 +131,9 @@ __device__ __forceinline__ float weights(const uint32_t (&s)[4][32], float c, fl
     for (int k = 0; k < 16; ++k) {
       const f32x2 x = fma2(pack2u(s[q][2 * k], s[q][2 * k + 1]), c2, sub2);
       float lo, hi;
-      if (!EDGE && (k & 7) >= 8 - kPolyOf8) {
-        poly_ex2(x, lo, hi);
-      } else {
-        unpack2(x, lo, hi);
-        lo = ex2(lo);
-        hi = ex2(hi);
-      }
+      unpack2(x, lo, hi);
+      lo = ex2(lo);
+      hi = ex2(hi);
       sum[k & 1] = add2(sum[k & 1], pack2(lo, hi));
       p[k] = pack_bf16(lo, hi);
     }
@@ -191,29 +172,28 @@ __device__ __forceinline__ int tiles_of(const Piece& p, int per, int causal) {
   const Rows a = rows_of(p, 0, per, causal), b = rows_of(p, 1, per, causal);
   return max(a.tiles, b.tiles);
 }
-// The piece number `index` found by one lane alone (find_piece takes a warp).
-__device__ __forceinline__ bool piece_by_lane(const PromptArgs& a, int rows, int index, Piece& out) {
-  for (int s = a.S - 1; s >= 0; --s) {
+// before[k]: tiles of keys of the pieces 0 .. k - 1; returns those of all `pieces`.  By one warp; bounds: scratch of S words.
+__device__ __forceinline__ int sum_tiles(const PromptArgs& a, int per, int pieces, int4* bounds, int32_t* before) {
+  const int lane = threadIdx.x & 31;
+  for (int s = lane; s < a.S; s += 32) {
     Piece p;
     if (!sequence(a, s, p)) report(a.status, DEV_BAD_INDEX);
-    const int n = (p.nq + rows - 1) / rows;
-    if (index < n) {
-      out = p;
-      out.first = (n - 1 - index) * rows;
-      return true;
-    }
-    index -= n;
+    bounds[s] = make_int4(p.q0, p.nq, p.k0, p.nk);
   }
-  return false;
-}
-// before[k]: tiles of the pieces 0 .. k - 1, by one warp; returns the sum over all `pieces`.
-__device__ __forceinline__ int sum_tiles(const PromptArgs& a, int per, int pieces, int32_t* before) {
-  const int lane = threadIdx.x & 31;
+  __syncwarp();
   int sum = 0;
   for (int k0 = 0; k0 < pieces; k0 += 32) {
-    Piece p;
     const int k = k0 + lane;
-    const int n = k < pieces && piece_by_lane(a, 2 * per, k, p) ? tiles_of(p, per, a.causal) : 0;
+    int n = 0, left = k;
+    for (int s = a.S - 1; s >= 0 && k < pieces; --s) {     // (the order is find_piece's)
+      const int4 q = bounds[s];
+      const int tiles = (q.y + 2 * per - 1) / (2 * per);
+      if (left < tiles) {
+        n = tiles_of({q.x, q.y, q.z, q.w, (tiles - 1 - left) * 2 * per}, per, a.causal);
+        break;
+      }
+      left -= tiles;
+    }
     int x = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -227,6 +207,8 @@ __device__ __forceinline__ int sum_tiles(const PromptArgs& a, int per, int piece
   __syncwarp();
   return sum;
 }
+// A part: for each 4 columns the values of its 256 rows, then the rows' maxima, then their sums (neighbouring rows are
+// neighbouring lanes of the kernels).
 __host__ __device__ constexpr int64_t part_floats(int d) { return (int64_t)2 * kTile * (d + 2); }
 
 template <int D>
@@ -431,7 +413,8 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     int e0 = 0, g = 0, number = blockIdx.x, round = 0;
     int64_t at = 0, end = 0;
     if (chief && least > 0) {
-      const int64_t total = (int64_t)sum_tiles(a, per, pieces, sh.before) * a.Hk, run = run_of(total, gridDim.x, least);
+      const int64_t total = (int64_t)sum_tiles(a, per, pieces, reinterpret_cast<int4*>(ring), sh.before) * a.Hk, run = run_of(total, gridDim.x, least);
+      fence_proxy_async();                                 // (the ring's place, which the copies get with the first task)
       at = (int64_t)blockIdx.x * run;
       end = min(at + run, total);
     }
@@ -519,6 +502,8 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     const int i = warp >> 2, r = threadIdx.x & 127;
     const uint32_t at = tmem + ((uint32_t)(32 * (warp & 3)) << 16), at_s = at + 128 * i, at_o = at + kColO + 128 * i;
     const float c = a.scale * kLog2e;
+    // (whole sectors where rows are aligned to them: half as many stores of a row per lane)
+    const bool wide_stores = ((reinterpret_cast<uintptr_t>(a.Y) | (uintptr_t)(2 * a.y_stride)) & 31) == 0;
     bool ok = true;
     int turn = 0, took = 0, guards = 0;                    // tiles of keys and tasks of this tile of rows, guarded value tiles
     for (int t = 0; ok; ++t) {
@@ -535,7 +520,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         all = rows.all;
         sees = a.causal ? max(0, min(pc.nk, token + 1 + pc.nk - pc.nq)) : pc.nk;
       }
-      float m = -INFINITY, l = 0.f;
+      float m = -INFINITY, l = 0.f, limit = -INFINITY;
       for (int jj = 0; jj < n; ++jj) {
         const int j = from + jj;
         if (!(ok = wait_warp(&sh.s_full[i], (turn + jj) & 1))) break;
@@ -555,17 +540,21 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
               if (32 * q + k >= most) s[q][k] = 0xff800000u;
         }
         // The weights of all but the last quarter are taken with the maximum of the tiles before; the tile's own is found on
-        // the side.  Only where it is higher by 2^8 (or there is none before, or a NaN) they are taken again.
+        // the side.  Only where it is higher by 2^8 (or a NaN, or there is none before) they are taken again.
         float mx = -INFINITY, sum = 0.f;
-        if (jj == 0) mx = row_max(s);
-        else sum = edge ? weights<true, 0, kMost / 32>(s, c, reference(m, c), at_s, &mx) : weights<false, 0, kMost / 32>(s, c, reference(m, c), at_s, &mx);
-        if (__any_sync(0xffffffffu, !((mx - m) * c <= kRaise))) {
+        bool first = jj == 0;
+        while (true) {
+          if (first) mx = row_max(s);
+          else sum = weights<0, kMost / 32>(s, c, reference(m, c), at_s, &mx);
+          if (!__any_sync(0xffffffffu, first || mx > limit || (mx != mx && m == m))) break;
+          first = false;
           const float up = max3_nan(m, mx, mx);
           const float f = up == m || up == -INFINITY ? 1.f : ex2((m - up) * c);
           m = up;
+          limit = m == m ? m + kRaise / c : INFINITY;
           l *= f;
           if (jj > 0) {
-            // S of this tile was issued behind O of the tile before, so O is complete
+            // (S of this tile was issued behind O of the tile before, so O is complete)
 #pragma unroll
             for (int q = 0; q < D / 16; ++q) {
               float o[16];
@@ -576,12 +565,11 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
               tmem_st16(at_o + 16 * q, w);
             }
           }
-          sum = weights<true, 0, kMost / 32>(s, c, reference(m, c), at_s, nullptr);
         }
         tmem_st_wait();
         tc_fence_before();
         mbar_arrive(&sh.p_most[i]);
-        sum += edge ? weights<true, kMost / 32, 4>(s, c, reference(m, c), at_s, nullptr) : weights<false, kMost / 32, 4>(s, c, reference(m, c), at_s, nullptr);
+        sum += weights<kMost / 32, 4>(s, c, reference(m, c), at_s, nullptr);
         tmem_st_wait();
         tc_fence_before();
         mbar_arrive(&sh.p_ready[i]);
@@ -605,7 +593,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         const int h = hk * G + r % G;
         const float inv = slot >= 0 ? 1.f : l == 0.f ? 0.f : 1.f / l;
         __nv_bfloat16* Y = static_cast<__nv_bfloat16*>(a.Y) + row * a.y_stride + (int64_t)h * D;
-        float* part = parts + (int64_t)max(slot, 0) * part_floats(D) + (i * kTile + r) * D;
+        float* part = parts + (int64_t)max(slot, 0) * part_floats(D) + 4 * (i * kTile + r);
 #pragma unroll
         for (int q = 0; q < D / 32; ++q) {
           uint32_t o[32];
@@ -632,7 +620,14 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           }
           if (slot >= 0) {
 #pragma unroll
-            for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(part + 32 * q + k) = make_float4(y[k], y[k + 1], y[k + 2], y[k + 3]);
+            for (int k = 0; k < 32; k += 4)
+              *reinterpret_cast<float4*>(part + (32 * q + k) * 2 * kTile) = make_float4(y[k], y[k + 1], y[k + 2], y[k + 3]);
+          } else if (mine && wide_stores) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 16)
+              store32(Y + 32 * q + k, pack_bf16(y[k], y[k + 1]), pack_bf16(y[k + 2], y[k + 3]), pack_bf16(y[k + 4], y[k + 5]),
+                      pack_bf16(y[k + 6], y[k + 7]), pack_bf16(y[k + 8], y[k + 9]), pack_bf16(y[k + 10], y[k + 11]),
+                      pack_bf16(y[k + 12], y[k + 13]), pack_bf16(y[k + 14], y[k + 15]));
           } else if (mine) {
 #pragma unroll
             for (int k = 0; k < 32; k += 8)
@@ -657,17 +652,19 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   if (warp == kIssuer) tmem_dealloc(tmem, 512);
 }
 
-// ---- partial results of split pieces.  A warp per row, 32 rows to a CTA: nothing to do if one CTA had the whole piece, zeros
-// if its rows see no key; else the parts are brought to their common maximum and added in the order of the CTAs.
-constexpr int kJoinRows = 32, kJoinThreads = 256;
+// ---- partial results of split pieces: 32 rows to a CTA, a row per lane, a share of the columns per warp.  Nothing to do if one
+// CTA had the whole piece, zeros if its rows see no key; else the parts are brought to their common maximum and added in the
+// order of the CTAs.
+constexpr int kJoinRows = 32, kJoinWarps = 8;
 template <int D>
-__global__ void __launch_bounds__(kJoinThreads) prompt_join_kernel(const PromptArgs a, int pieces, int least, int ctas, const float* parts) {
+__global__ void __launch_bounds__(32 * kJoinWarps) prompt_join_kernel(const PromptArgs a, int pieces, int least, int ctas, const float* parts) {
+  __shared__ int4 bounds[kMostSplit];
   __shared__ int32_t before[kMostSplit + 1];
   __shared__ Piece shared_piece;
   __shared__ int found;
   const int G = a.H / a.Hk, per = kTile / G, k = blockIdx.x / a.Hk, hk = blockIdx.x % a.Hk;
   if (threadIdx.x < 32) {
-    sum_tiles(a, per, pieces, before);
+    sum_tiles(a, per, pieces, bounds, before);
     Piece p;
     const bool ok = find_piece(a, 2 * per, k, p);
     if (threadIdx.x == 0) { found = ok; shared_piece = p; }
@@ -677,39 +674,55 @@ __global__ void __launch_bounds__(kJoinThreads) prompt_join_kernel(const PromptA
   const Piece pc = shared_piece;
   const int U = before[k + 1] - before[k];
   const int64_t run = run_of((int64_t)before[pieces] * a.Hk, ctas, least), g0 = (int64_t)before[k] * a.Hk + (int64_t)hk * U;
-  const int c0 = (int)(g0 / run), c1 = U > 0 ? (int)((g0 + U - 1) / run) : c0;
+  const int c0 = (int)quotient(g0, run), c1 = U > 0 ? (int)quotient(g0 + U - 1, run) : c0;
   if (U > 0 && c0 == c1) return;
-  pdl_wait();                                              // the parts come from the kernel before
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr int kPer = D / 32;
-  for (int r = blockIdx.y * kJoinRows + warp; r < (int)(blockIdx.y + 1) * kJoinRows; r += kJoinThreads / 32) {
-    const int i = r / kTile, x = r % kTile, token = pc.first + i * per + x / G;
-    if (x >= per * G || token >= pc.nq) continue;
-    float m = -INFINITY, l = 0.f, y[kPer] = {};
-    auto slot = [&](int n) { return parts + (int64_t)(2 * (c0 + n) + (n == 0)) * part_floats(D); };
-    const int n = U > 0 ? c1 - c0 + 1 : 0;
-    for (int p = 0; p < n; ++p) m = fmaxf(m, ld_after_wait(slot(p) + 2 * kTile * D + r));
-    const float use = m == -INFINITY ? 0.f : m;
-    for (int p = 0; p < n; ++p) {
-      const float* s = slot(p);
-      const float top = ld_after_wait(s + 2 * kTile * D + r), sum = ld_after_wait(s + 2 * kTile * D + 2 * kTile + r);
-      float v[kPer];
+  const int r = blockIdx.y * kJoinRows + lane, i = r / kTile, x = r % kTile, token = pc.first + i * per + x / G;
+  if (x >= per * G || token >= pc.nq) return;
+  pdl_wait();                                              // the parts come from the kernel before
+  constexpr int kPer = D / kJoinWarps, kBatch = 4;         // columns of a lane, parts in flight together
+  const int n = U > 0 ? c1 - c0 + 1 : 0;
+  auto slot = [&](int p) { return parts + (int64_t)(2 * (c0 + p) + (p == 0)) * part_floats(D); };
+  float m = -INFINITY, l = 0.f, y[kPer] = {};
+#pragma unroll 8
+  for (int p = 0; p < n; ++p) m = fmaxf(m, ld_after_wait(slot(p) + 2 * kTile * D + r));
+  const float use = m == -INFINITY ? 0.f : m;
+  for (int p0 = 0; p0 < n; p0 += kBatch) {
+    float top[kBatch], sum[kBatch];
+    float4 v[kBatch][kPer / 4];
 #pragma unroll
-      for (int q = 0; q < kPer; ++q) v[q] = ld_after_wait(s + r * D + lane + 32 * q);
-      const float w = exp2f(top - use);
-      if (w == 0.f) continue;
-      l = fmaf(w, sum, l);
+    for (int b = 0; b < kBatch; ++b) {
+      top[b] = -INFINITY;
+      if (p0 + b >= n) continue;
+      const float* s = slot(p0 + b);
+      top[b] = ld_after_wait(s + 2 * kTile * D + r);
+      sum[b] = ld_after_wait(s + 2 * kTile * D + 2 * kTile + r);
 #pragma unroll
-      for (int q = 0; q < kPer; ++q) y[q] = fmaf(w, v[q], y[q]);
+      for (int q = 0; q < kPer / 4; ++q) v[b][q] = ld_after_wait(reinterpret_cast<const float4*>(s + (warp * kPer + 4 * q) * 2 * kTile + 4 * r));
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int64_t row = (int64_t)pc.q0 + token;
-    const int h = hk * G + x % G;
-    __nv_bfloat16* Y = static_cast<__nv_bfloat16*>(a.Y) + row * a.y_stride + (int64_t)h * D;
 #pragma unroll
-    for (int q = 0; q < kPer; ++q) Y[lane + 32 * q] = __float2bfloat16_rn(y[q] * inv);
-    if (a.lse && lane == 0) a.lse[row * a.H + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+    for (int b = 0; b < kBatch; ++b) {
+      const float w = exp2f(top[b] - use);
+      if (w == 0.f) continue;
+      l = fmaf(w, sum[b], l);
+#pragma unroll
+      for (int q = 0; q < kPer / 4; ++q) {
+        y[4 * q] = fmaf(w, v[b][q].x, y[4 * q]);
+        y[4 * q + 1] = fmaf(w, v[b][q].y, y[4 * q + 1]);
+        y[4 * q + 2] = fmaf(w, v[b][q].z, y[4 * q + 2]);
+        y[4 * q + 3] = fmaf(w, v[b][q].w, y[4 * q + 3]);
+      }
+    }
   }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int64_t row = (int64_t)pc.q0 + token;
+  const int h = hk * G + x % G;
+  __nv_bfloat16* Y = static_cast<__nv_bfloat16*>(a.Y) + row * a.y_stride + (int64_t)h * D + warp * kPer;
+#pragma unroll
+  for (int q = 0; q < kPer; q += 8)
+    *reinterpret_cast<uint4*>(Y + q) = make_uint4(pack_bf16(y[q] * inv, y[q + 1] * inv), pack_bf16(y[q + 2] * inv, y[q + 3] * inv),
+                                                  pack_bf16(y[q + 4] * inv, y[q + 5] * inv), pack_bf16(y[q + 6] * inv, y[q + 7] * inv));
+  if (a.lse && warp == 0) a.lse[row * a.H + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 // Whether the block's registers at launch cover the shares that its warps ask for (or they would wait for good).
@@ -747,12 +760,12 @@ avq_status launch(const PromptArgs& a, cudaStream_t st) {
   const int64_t pieces = most_pieces(a.Tq, a.S, 2 * per), all = pieces * a.Hk;
   if (all >= (int64_t)1 << 30) return AVQ_ERR_UNSUPPORTED;
   // Pieces that cannot fill the GPU, over keys that can be long, are split, if the caller's workspace holds the parts.
-  const bool split = a.parts && all <= kSplitBelow && pieces <= kMostSplit && a.Tk >= kSplitKeys;
+  const bool split = a.parts && all <= kSplitBelow && pieces <= kMostSplit && a.S <= kMostSplit && a.Tk >= kSplitKeys;
   const int grid = split ? sms : (int)(all < sms ? all : sms), least = split ? kLeastTiles : 0;
   prompt_tc_kernel<D><<<grid, kThreads, prompt_smem<D>(), st>>>(tmQ, tmK, tmV, a, (int)pieces, least, a.parts);
   if (cudaGetLastError() != cudaSuccess) return AVQ_ERR_CUDA;
   if (!split) return AVQ_OK;
-  return cuda_ok(launch_pdl(prompt_join_kernel<D>, dim3((unsigned)all, 2 * kTile / kJoinRows), dim3(kJoinThreads), 0, st, true, a, (int)pieces,
+  return cuda_ok(launch_pdl(prompt_join_kernel<D>, dim3((unsigned)all, 2 * kTile / kJoinRows), dim3(32 * kJoinWarps), 0, st, true, a, (int)pieces,
                             least, grid, (const float*)a.parts));
 }
 
