@@ -295,8 +295,10 @@ typedef struct {
 } avq_heads;
 
 /* Envelope of the exact operators.
- *   CUDA-core kernels (AVQ_FLAG_SIMT; float32 prompts always): d % 8 == 0, 8 <= d <= 256, any finite scale.
- *   Tensor-core kernels: d in {64, 128}, scale > 0; avq_prompt_attend (bfloat16): H / Hk <= 128.
+ *   CUDA-core kernels (AVQ_FLAG_SIMT): d % 8 == 0, 8 <= d <= 256, any finite scale.
+ *   Tensor-core kernels: d in {64, 128}, scale > 0; avq_prompt_attend in bfloat16: H / Hk <= 128.
+ *   avq_prompt_attend in float32 takes what the CUDA cores take without the flag too, and runs d in {64, 128} on the tensor
+ *   cores, to the same precision (three products of the operands' high and low parts).
  *   Caches: page a multiple of 16, 16..1024; pages * page < 2^31; in 4 bits d % 32 == 0.
  */
 

@@ -313,6 +313,7 @@ avq_status cache_read(const ReadArgs& a, int dtype, int bits, cudaStream_t st);
 avq_status simt_prompt(const PromptArgs& a, int dtype, cudaStream_t st);
 avq_status simt_cached(const CachedArgs& a, int dtype, int bits, cudaStream_t st);
 avq_status tc_prompt(const PromptArgs& a, cudaStream_t st);
+avq_status tc_prompt_f32(const PromptArgs& a, cudaStream_t st);
 constexpr int kPromptCtas = 148;                           // (more SMs than that are not asked for)
 size_t tc_prompt_part_bytes(int d);
 avq_status tc_cached(const CachedArgs& a, int dtype, int bits, cudaStream_t st);

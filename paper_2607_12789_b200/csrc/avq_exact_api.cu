@@ -1,5 +1,5 @@
 // C ABI of the exact operators: argument validation and dispatch.  The kernels live in avq_exact_simt.cu (CUDA cores,
-// and the joining of split sequences), avq_tc_prompt.cu and avq_tc_cached.cu (tensor cores) and avq_cache.cu (rows into and out of a cache).
+// and the joining of split sequences), avq_tc_prompt.cu, avq_tc_prompt_f32.cu and avq_tc_cached.cu (tensor cores) and avq_cache.cu (rows into and out of a cache).
 #include "avq_exact.cuh"
 
 namespace avq {
@@ -103,7 +103,8 @@ avq_status avq_prompt_attend(const avq_heads* heads, const void* Q, int64_t q_st
                         workspace_bytes > 256 && workspace_bytes >= avq_prompt_split_bytes(heads)
                             ? reinterpret_cast<float*>(static_cast<char*>(workspace) + 256) : nullptr};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return h.dtype == AVQ_BF16 && tensor_path(h) ? tc_prompt(a, st) : simt_prompt(a, h.dtype, st);
+  if (!tensor_path(h) || (h.dtype == AVQ_F32 && h.d != 64 && h.d != 128)) return simt_prompt(a, h.dtype, st);
+  return h.dtype == AVQ_F32 ? tc_prompt_f32(a, st) : tc_prompt(a, st);
 }
 
 size_t avq_cache_bytes(const avq_cache* cache) {
