@@ -89,6 +89,9 @@ __device__ __forceinline__ uint32_t codes_at(uint32_t w, int i) {
 // c 2^-24 of the codes at bits 4 (i - i % 2) of both halves, c 2^-20 of those at bits 4 i (odd i)
 __device__ __forceinline__ uint32_t subnormal_codes(uint32_t w, int i) { return (w >> (8 * (i >> 1))) & ((i & 1) ? 0x00f000f0u : 0x000f000fu); }
 __device__ __forceinline__ float tf32_high(float x) { return __uint_as_float(__float_as_uint(x) & 0xffffe000u); }
+// The low part of a value with the high part h.  An infinity is its own high part; its low part is a number so far below
+// the largest that its products stay finite (those of finite values are smaller still), not a NaN.
+__device__ __forceinline__ float tf32_low(float x, float h) { return fminf(x - h, 1e36f); }
 // The low part of a weight with the high part h, never zero beside one: 2^-30 of it at least, so that an infinite value times
 // it is that infinity and no NaN.
 __device__ __forceinline__ float tf32_low_weight(float p, float h) { return fmaxf(p - h, h * 9.3132257e-10f); }

@@ -411,7 +411,7 @@ struct Warp {
             for (int e = 0; e < 4; ++e) {
               const float f = __uint_as_float(h[e]), fh = tf32_high(f);
               h[e] = __float_as_uint(fh);
-              x[e] = isfinite(f) ? __float_as_uint(f - fh) : 0u;
+              x[e] = __float_as_uint(tf32_low(f, fh));
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
