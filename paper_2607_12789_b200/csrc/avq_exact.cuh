@@ -179,7 +179,10 @@ inline int64_t most_pieces(int64_t T, int64_t S, int64_t rows) { return T / rows
 // (sequence, key head, block, unit), are dealt out in equal runs to the CTAs, whatever the lengths: a CTA finishes the
 // segments that lie inside its run and leaves partial results of the at most two that do not, its first in slot 2 c,
 // its last in slot 2 c + 1.  join_kernel merges those in the order of the CTAs.
-constexpr int kRows = 16, kUnit = 16;
+// A segment also costs a CTA its queries, the start of its copies and the end of its sums, whatever its length: about as much
+// as kSetup units, which stand before its own (six sequences of which one has 4 tokens, float32: 52.6 us
+// without, 41.4 with 8, 30.5 with 16, 29.3 with 32, which costs a step of 64 sequences 2 %).
+constexpr int kRows = 16, kUnit = 16, kSetup = 16;
 constexpr int kMaxCtas = 148 * 4;                          // (more SMs than that are not asked for)
 __host__ __device__ constexpr int64_t slot_floats(int d) { return (int64_t)kRows * (d + 2); }
 
@@ -190,6 +193,7 @@ __device__ __forceinline__ int clipped_len(const CachedArgs& a, int b, bool tell
   return n < 0 ? 0 : (int64_t)n > most ? (int)most : n;
 }
 __device__ __forceinline__ int units_of(int len) { return (len + kUnit - 1) / kUnit; }
+__device__ __forceinline__ int weight_of(int units) { return units > 0 ? units + kSetup : 0; }
 __device__ __forceinline__ int segments_per_sequence(const CachedArgs& a) {
   return a.Hk * ((a.nq * (a.H / a.Hk) + kRows - 1) / kRows);
 }
@@ -239,22 +243,27 @@ __device__ __forceinline__ bool walk_next(const CachedArgs& a, Walk& w, Segment&
   const int per = segments_per_sequence(a), blocks = per / a.Hk;
   const Place p = w.place[turn & 1];
   const int64_t end = w.end;
-  if (p.at >= end) return false;
-  int64_t before = p.before;
-  int b = p.b, len = clipped_len(a, b, false), U = units_of(len);
-  while (p.at >= before + (int64_t)U * per) {              // (ends: at < end <= all units)
-    before += (int64_t)U * per;
-    len = clipped_len(a, ++b, false);
-    U = units_of(len);
+  int64_t at = p.at, before = p.before;
+  int b = p.b, len = clipped_len(a, b, false), U = units_of(len), W = weight_of(U);
+  while (at < end) {                                       // (a run's last bit may be a setup alone: that segment is the next CTA's)
+    while (at >= before + (int64_t)W * per) {              // (ends: at < end <= the weight of all)
+      before += (int64_t)W * per;
+      len = clipped_len(a, ++b, false);
+      U = units_of(len);
+      W = weight_of(U);
+    }
+    const int64_t rel = at - before;
+    const int seg = (int)quotient(rel, W), x = (int)(rel - (int64_t)seg * W), take = (int)min((int64_t)(W - x), end - at);
+    at += take;
+    sg.unit = max(0, x - kSetup);
+    sg.n = x + take - kSetup - sg.unit;
+    if (sg.n <= 0) continue;
+    sg.b = b; sg.hk = seg / blocks; sg.block = seg % blocks; sg.len = len;
+    sg.units = U;
+    if (threadIdx.x == 0) w.place[(turn + 1) & 1] = {at, before, b};
+    return true;
   }
-  const int64_t rel = p.at - before;
-  const int seg = (int)quotient(rel, U);
-  sg.b = b; sg.hk = seg / blocks; sg.block = seg % blocks; sg.len = len;
-  sg.unit = (int)(rel - (int64_t)seg * U);
-  sg.units = U;
-  sg.n = (int)min((int64_t)(U - sg.unit), end - p.at);
-  if (threadIdx.x == 0) w.place[(turn + 1) & 1] = {p.at + sg.n, before, b};
-  return true;
+  return false;
 }
 // Sum of `v` over the threads before this one; `total`: over all of them.
 __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* scratch, int64_t& total) {
@@ -279,13 +288,13 @@ __device__ __forceinline__ bool walk_begin(const CachedArgs& a, int least, Walk&
   int64_t total = 0;
   if (a.B > (int)blockDim.x) {                             // more than one scan: all lengths once for their sum
     int64_t mine = 0;
-    for (int b = threadIdx.x; b < a.B; b += blockDim.x) mine += units_of(clipped_len(a, b, false));
+    for (int b = threadIdx.x; b < a.B; b += blockDim.x) mine += weight_of(units_of(clipped_len(a, b, false)));
     total = block_sum(mine, w.scratch) * per;
   }
   int64_t before = 0;
   for (int b0 = 0; b0 < a.B; b0 += blockDim.x) {           // the sequence that holds the run's first unit
     const int b = b0 + threadIdx.x;
-    const int64_t u = b < a.B ? (int64_t)units_of(clipped_len(a, b, blockIdx.x == 0)) * per : 0;
+    const int64_t u = b < a.B ? (int64_t)weight_of(units_of(clipped_len(a, b, blockIdx.x == 0))) * per : 0;
     int64_t all;
     const int64_t base = before + block_scan(u, w.scratch, all);
     if (a.B <= (int)blockDim.x) total = all;

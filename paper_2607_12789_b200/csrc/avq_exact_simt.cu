@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const CachedArgs a, 
   if (q >= a.nq * G) return;
   int64_t all = 0, before = 0;
   for (int i = threadIdx.x; i < a.B; i += kJoinThreads) {
-    const int u = units_of(clipped_len(a, i, false));
+    const int u = weight_of(units_of(clipped_len(a, i, false)));
     all += u;
     if (i < b) before += u;
   }
@@ -381,8 +381,8 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const CachedArgs a, 
     if (a.lse && threadIdx.x == 0) a.lse[token * a.H + h] = -INFINITY;
     return;
   }
-  const int64_t run = run_of(all, ctas, least), g0 = before + (int64_t)seg * U;
-  const int c0 = (int)(g0 / run), c1 = (int)((g0 + U - 1) / run);
+  const int64_t run = run_of(all, ctas, least), g0 = before + (int64_t)seg * weight_of(U) + kSetup;   // the segment's first unit
+  const int c0 = (int)quotient(g0, run), c1 = (int)quotient(g0 + U - 1, run);
   if (c0 == c1) return;
   tc::pdl_wait();                                          // the slots come from the kernel before
   const int64_t size = slot_floats(d);
