@@ -456,7 +456,7 @@ struct Warp {
           float x = top[n][e];
 #pragma unroll
           for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-          x = fmaxf(x, m[n][e]);
+          if (!(x > limit[n][e])) continue;                // (each column by its own logits alone: roundings too)
           const float f = x == -INFINITY ? 1.f : ex2((m[n][e] - x) * c);
           m[n][e] = x;
           limit[n][e] = x + kRaise / c;

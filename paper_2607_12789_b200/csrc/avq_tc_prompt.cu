@@ -546,9 +546,11 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         while (true) {
           if (first) mx = row_max(s);
           else sum = weights<0, kMost / 32>(s, c, reference(m, c), at_s, &mx);
-          if (!__any_sync(0xffffffffu, first || mx > limit || (mx != mx && m == m))) break;
+          // (each row by its own logits alone: what others hold, and whether they are raised, does not change its roundings)
+          const bool raise = first || mx > limit || (mx != mx && m == m);
+          if (!__any_sync(0xffffffffu, raise)) break;
           first = false;
-          const float up = max3_nan(m, mx, mx);
+          const float up = raise ? max3_nan(m, mx, mx) : m;
           const float f = up == m || up == -INFINITY ? 1.f : ex2((m - up) * c);
           m = up;
           limit = m == m ? m + kRaise / c : INFINITY;

@@ -43,6 +43,15 @@ def test_unusable_heads_are_refused(lib, kw, want):
     assert _prompt(lib, h, qs=1 << 20, ys=1 << 20) == want
 
 
+def test_room_for_parts(lib):
+    """Two parts for each of 148 CTAs: 256 rows of d values, a maximum and a sum; none where no kernel splits."""
+    assert lib.avq_prompt_workspace_bytes(_heads()) == 256
+    assert lib.avq_prompt_split_bytes(_heads()) == 256 + 4 * 2 * 148 * 256 * 66
+    assert lib.avq_prompt_split_bytes(_heads(d=128)) == 256 + 4 * 2 * 148 * 256 * 130
+    assert lib.avq_prompt_split_bytes(_heads(dtype=0)) == lib.avq_prompt_split_bytes(_heads(flags=2)) == 256
+    assert lib.avq_prompt_split_bytes(_heads(d=96)) == 0
+
+
 @pytest.mark.parametrize("kw,want", [
     (dict(S=-1), 2), (dict(Tq=-1), 2), (dict(Tk=-1), 2), (dict(ck=0), 2), (dict(qs=248), 2), (dict(ks=120), 2), (dict(ys=0), 2),
     (dict(Q=0), 1), (dict(K=0), 1), (dict(V=0), 1), (dict(Y=0), 1), (dict(cq=0), 1), (dict(Q=ODD), 4), (dict(V=ODD), 4),

@@ -187,6 +187,90 @@ def test_a_captured_prompt_follows_its_inputs(dtype, flags):
     att.check()
 
 
+@pytest.mark.parametrize("dtype,d", [(BF16, 64), (BF16, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "all"])
+def test_prompt_of_many_sequences(dtype, d, causal):
+    """Far more tiles than the GPU has processors: a CTA takes one after another, long and short, with and without keys."""
+    lens = [(37 * i) % 300 for i in range(70)] + [0, 1, 513]
+    keys = [n + (i % 3) * 40 if i % 7 else max(n - 60, 0) for i, n in enumerate(lens)]
+    _run_prompt(dtype, 0, 8, 8, d, lens, lens, causal, 13)
+    _run_prompt(dtype, 0, 24, 8, d, lens, keys, causal, 14)
+
+
+SPLIT = {"piece": ([64], [5000]), "one": ([1], [2500]), "several": ([3, 0, 70, 1], [2100, 3000, 64, 0]), "ahead": ([200, 30], [150, 4000]),
+         "long": ([256], [20000])}
+
+
+@pytest.mark.parametrize("d,heads", [(64, (4, 1)), (128, (2, 2)), (128, (16, 2)), (64, (3, 1))])
+@pytest.mark.parametrize("lens", list(SPLIT))
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "all"])
+def test_few_queries_over_many_keys(d, heads, lens, causal):
+    """Calls that are split along the keys, against 64 bits, twice alike, and near what a call without room for parts gives."""
+    (H, Hk), (lq, lk) = heads, SPLIT[lens]
+    _run_prompt(BF16, 0, H, Hk, d, lq, lk, causal, 15)
+    g = _gen(16)
+    Q, K, V = (_randn(g, n, m, d, dtype=BF16) for n, m in ((sum(lq), H), (sum(lk), Hk), (sum(lk), Hk)))
+    cu = _ints(_ends(lq)), _ints(_ends(lk))
+    whole = binding.ExactAttention(H, Hk, d, causal=causal, split=False)
+    parts = binding.ExactAttention(H, Hk, d, causal=causal)
+    assert whole.workspace.numel() == 256 and parts.workspace.numel() > 2 ** 20
+    parts.workspace[256:].fill_(255)
+    a, b, c = whole(Q, K, V, *cu), parts(Q, K, V, *cu), parts(Q, K, V, *cu)
+    assert torch.equal(b, c)
+    # each is within half a bfloat16 step of a weight times the largest value of the exact rows, and half a step of its own
+    assert ((a.float() - b.float()).abs() <= 2 * (2.0 ** -8 * V.abs().max().item() + 2.0 ** -8 * a.float().abs()) + 1e-3).all()
+
+
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+def test_split_calls_keep_what_is_not_seen_out(bad):
+    g = _gen(18)
+    H, Hk, d, lq, lk = 4, 1, 128, [20, 40], [3000, 2500]
+    Q, K, V = (_randn(g, n, m, d, dtype=BF16) for n, m in ((80, H), (5700, Hk), (5700, Hk)))
+    att = binding.ExactAttention(H, Hk, d)
+    cq, ck = _ints([5, 25, 65]), _ints([100, 3100, 5600])
+    clean = att(Q, K, V, cq, ck)
+    K2, V2 = K.clone(), V.clone()
+    for x in (K2, V2):
+        x[:100], x[5600:], x[3100 - 5] = bad, bad, bad       # the last five queries but one of the first sequence see that key
+    Y = torch.full((80, H, d), 7.0, dtype=BF16, device="cuda")
+    att(Q, K2, V2, cq, ck, Y=Y)
+    assert torch.equal(Y[5:20], clean[5:20]) and torch.equal(Y[25:65], clean[25:65])
+    assert torch.isnan(Y[20:25].float()).any(-1).any(-1).all() and (Y[:5] == 7).all() and (Y[65:] == 7).all()
+    V2 = V.clone()
+    V2[3100 - 5, 0, 9] = bad
+    Y = att(Q, K, V2, cq, ck)
+    want = clean.clone()
+    want[20:25, :, 9] = bad
+    assert ((Y == want) | (torch.isnan(Y.float()) & torch.isnan(want.float())))[5:65].all()
+    att.check()
+
+
+def test_split_calls_leave_unusable_bounds_out_and_follow_a_captured_graph():
+    g = _gen(19)
+    Q, K, V = (_randn(g, n, m, 64, dtype=BF16) for n, m in ((60, 4), (6000, 2), (6000, 2)))
+    att = binding.ExactAttention(4, 2, 64)
+    good = att(Q, K, V, _ints([0, 30, 60]), _ints([0, 2500, 6000]))
+    att.check()
+    Y = torch.full_like(Q, 5.0)
+    att(Q, K, V, _ints([0, 30, 60]), _ints([0, 2500, 6001]), Y=Y)
+    with pytest.raises(binding.AvqError, match="AVQ_ERR_INDEX"):
+        att.check()
+    assert torch.equal(Y[:30], good[:30]) and (Y[30:] == 5).all()
+    cq, ck = _ints([0, 30, 60]), _ints([0, 2500, 6000])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        att(Q, K, V, cq, ck, Y=Y)
+    for a, b in (([0, 1, 60], [0, 6000, 6000]), ([0, 60, 60], [0, 5500, 5600]), ([10, 20, 50], [0, 64, 4000])):
+        cq.copy_(_ints(a))
+        ck.copy_(_ints(b))
+        Y.fill_(3.0)
+        graph.replay()
+        want = torch.full_like(Q, 3.0)
+        att(Q, K, V, cq, ck, Y=want)
+        assert torch.equal(Y, want)
+    att.check()
+
+
 # ---------------------------------------------------------------- the cache
 def _cache(pages, page, Hk, d, dtype, bits, g, fill=True):
     c = binding.PagedCache.empty(pages, page, Hk, d, dtype=dtype, bits=bits)
