@@ -105,21 +105,20 @@ __device__ __forceinline__ uint32_t q4_encode8(const float (&v)[8], uint32_t& pa
   const float step = __bfloat162float(stepb);
   pair = (uint32_t)__bfloat16_as_ushort(lob) | (uint32_t)__bfloat16_as_ushort(stepb) << 16;
   if (!(step > 0.f)) return 0;                             // (a NaN too: the group reads as NaN whatever its codes)
-  // Adding 1.5 * 2^23 rounds to the nearest integer (ties to even) and leaves it in the low bits.  By the approximate
-  // reciprocal a quotient up to 2^5 is off by less than 2^-17: only where one is next to a half all are divided out.
+  // Quotients as correctly rounded divisions have them, by Markstein's two steps from the reciprocal (ties of codes are
+  // common among bfloat16 values: a division for each that is next to one was three quarters of this kernel's
+  // instructions).  Adding 1.5 * 2^23 rounds to the nearest integer, ties to even, and leaves it in the low bits.
   constexpr float kMagic = 12582912.f;
-  float by, near = step < 1e-30f ? 1.f : 0.f;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(by) : "f"(step));
   uint32_t word = 0;
+  if (step >= 1e-30f) {
+    const float by = __frcp_rn(step);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float x = __fsub_rn(v[i], lo), t = __fmaf_rn(x, by, kMagic);
-    near = fmaxf(near, fabsf(__fmaf_rn(x, by, -__fsub_rn(t, kMagic))));
-    word += __float_as_uint(fminf(fmaxf(t, kMagic), kMagic + 15.f)) << (4 * i);   // (the magic number's own low bits are zero)
-  }
-  word -= kMagicSum;
-  if (!(near < 0.4999f)) {
-    word = 0;
+    for (int i = 0; i < 8; ++i) {
+      const float x = __fsub_rn(v[i], lo), q = __fmul_rn(x, by), c = __fmaf_rn(__fmaf_rn(-q, step, x), by, q);
+      word += __float_as_uint(fminf(fmaxf(__fadd_rn(c, kMagic), kMagic), kMagic + 15.f)) << (4 * i);   // (the magic number's own low bits are zero)
+    }
+    word -= kMagicSum;
+  } else {                                                 // (the reciprocal may be beyond the largest number)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float c = fminf(fmaxf(__fdiv_rn(__fsub_rn(v[i], lo), step), 0.f), 15.f);

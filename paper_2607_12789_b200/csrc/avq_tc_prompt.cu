@@ -32,7 +32,7 @@ constexpr int kTile = 128, kThreads = 384, kLoader = 8, kIssuer = 9, kGuards = 6
 constexpr int kMost = 96;                                  // weights of a tile that the product starts with
 constexpr int kReady = 8;                                  // value tiles that the guards can be ahead by, at least
 constexpr float kRaise = 8.f;
-constexpr int kSplitBelow = 148, kSplitKeys = 2048, kLeastTiles = 4;   // when pieces are split, and into parts of what size at least
+constexpr int kSplitBelow = 148, kSplitKeys = 2048, kLeastTiles = 4, kSetupTiles = 2;   // when pieces are split, and into parts of what size at least
 constexpr int kFewRegs = 80, kManyRegs = 208;              // per thread of warps 8-11, of warps 0-7
 template <int D> __host__ __device__ constexpr int ring_slots() { return D == 128 ? 5 : 10; }
 template <int D> __host__ __device__ constexpr int tile_bytes() { return kTile * D * 2; }
@@ -53,7 +53,7 @@ struct Shared {
   Task task[kTasks];
   uint32_t tmem;
   int abort_flag, wide[kTasks];
-  int32_t before[kMostSplit + 1];   // split calls: tiles of keys of the pieces before each
+  int32_t before[kMostSplit + 1];   // split calls: tiles of keys, with the setups, of the pieces before each
 };
 
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
@@ -167,12 +167,14 @@ __device__ __forceinline__ Rows rows_of(const Piece& p, int tile, int per, int c
 // sizes fall with the number, and going back and forth evens them out.
 // Few pieces (`run` > 0): all tiles of keys of all pieces and key heads, in that order, are dealt out in runs of `run`; a CTA
 // finishes what lies inside its run and leaves partial results of the at most two pieces that do not, its first in slot
-// 2 c, its last in slot 2 c + 1; prompt_join_kernel adds them in the order of the CTAs.
+// 2 c, its last in slot 2 c + 1; prompt_join_kernel adds them in the order of the CTAs.  What a piece costs whatever its
+// tiles (its first logits, its outputs) counts as kSetupTiles more, ahead of its own.
 __device__ __forceinline__ int tiles_of(const Piece& p, int per, int causal) {
   const Rows a = rows_of(p, 0, per, causal), b = rows_of(p, 1, per, causal);
   return max(a.tiles, b.tiles);
 }
-// before[k]: tiles of keys of the pieces 0 .. k - 1; returns those of all `pieces`.  By one warp; bounds: scratch of S words.
+// before[k]: tiles of keys, with the setups, of the pieces 0 .. k - 1; returns those of all `pieces`.  By one warp; bounds:
+// scratch of S words.
 __device__ __forceinline__ int sum_tiles(const PromptArgs& a, int per, int pieces, int4* bounds, int32_t* before) {
   const int lane = threadIdx.x & 31;
   for (int s = lane; s < a.S; s += 32) {
@@ -190,6 +192,7 @@ __device__ __forceinline__ int sum_tiles(const PromptArgs& a, int per, int piece
       const int tiles = (q.y + 2 * per - 1) / (2 * per);
       if (left < tiles) {
         n = tiles_of({q.x, q.y, q.z, q.w, (tiles - 1 - left) * 2 * per}, per, a.causal);
+        n += n > 0 ? kSetupTiles : 0;
         break;
       }
       left -= tiles;
@@ -423,20 +426,21 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       task.index = -1;
       task.slot = -1;
       if (least > 0) {
-        if (at < end) {
+        while (at < end && task.index < 0) {
           int k = 0;                                       // the last piece that begins at or before `at` and has tiles
           for (int x = lane; x < pieces; x += 32)
             if ((int64_t)sh.before[x] * a.Hk <= at && sh.before[x + 1] > sh.before[x]) k = max(k, x);
           k = __reduce_max_sync(0xffffffffu, k);
+          const int W = sh.before[k + 1] - sh.before[k], U = W - kSetupTiles;
+          const int rel = (int)(at - (int64_t)sh.before[k] * a.Hk), x = rel % W, take = (int)min((int64_t)(W - x), end - at);
+          at += take;
+          if (x + take <= kSetupTiles) continue;           // (the setup alone: the piece is the next CTA's)
           find_piece(a, 2 * per, k, task.piece);
-          const int U = sh.before[k + 1] - sh.before[k];
-          const int rel = (int)(at - (int64_t)sh.before[k] * a.Hk);
           task.index = k;
-          task.hk = rel / U;
-          task.from = rel % U;
-          task.to = (int)min((int64_t)U, task.from + (end - at));
+          task.hk = rel / W;
+          task.from = max(0, x - kSetupTiles);
+          task.to = x + take - kSetupTiles;
           if (task.from > 0 || task.to < U) task.slot = 2 * blockIdx.x + (task.from == 0);
-          at += task.to - task.from;
         }
       } else {
         if (find_piece(a, 2 * per, number / a.Hk, task.piece)) {
@@ -674,8 +678,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) prompt_join_kernel(const Prom
   __syncthreads();
   if (!found) return;
   const Piece pc = shared_piece;
-  const int U = before[k + 1] - before[k];
-  const int64_t run = run_of((int64_t)before[pieces] * a.Hk, ctas, least), g0 = (int64_t)before[k] * a.Hk + (int64_t)hk * U;
+  const int W = before[k + 1] - before[k], U = max(0, W - kSetupTiles);
+  const int64_t run = run_of((int64_t)before[pieces] * a.Hk, ctas, least), g0 = (int64_t)before[k] * a.Hk + (int64_t)hk * W + kSetupTiles;
   const int c0 = (int)quotient(g0, run), c1 = U > 0 ? (int)quotient(g0 + U - 1, run) : c0;
   if (U > 0 && c0 == c1) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
