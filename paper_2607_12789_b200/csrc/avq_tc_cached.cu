@@ -39,8 +39,10 @@ enum Rows { kBf16 = 0, kQ4 = 1, kF32 = 2 };
 template <int MODE, int D> __host__ __device__ constexpr int unit_bytes() {
   return MODE == kQ4 ? 2 * kUnit * (D / 2 + D / 8) : 2 * kUnit * D * (MODE == kF32 ? 4 : 2);
 }
-template <int MODE, int D> __host__ __device__ constexpr int stages() { return MODE == kQ4 ? 6 : MODE == kBf16 && D == 64 ? 5 : 3; }
-template <int MODE, int D, int NT> __host__ __device__ constexpr int ctas_per_sm() { return MODE == kQ4 && NT == 1 ? 3 : MODE == kF32 && D == 128 ? 1 : 2; }
+// (4 bits: two CTAs to an SM, units in pairs and eight of them in a warp's ring 39.1 us for two long sequences; three CTAs with
+// six 41.9, which leave the pairs too few registers, with seven 47.3.)
+template <int MODE, int D> __host__ __device__ constexpr int stages() { return MODE == kQ4 ? 8 : MODE == kBf16 && D == 64 ? 5 : 3; }
+template <int MODE, int D, int NT> __host__ __device__ constexpr int ctas_per_sm() { return MODE == kF32 && D == 128 ? 1 : 2; }
 // Query fragments in shared memory: float32 queries only (their parts would take too many registers).
 template <int MODE, int D, int NT, int PARTS> __host__ __device__ constexpr int query_bytes() {
   return MODE == kF32 ? (D / 8) * NT * 32 * 16 : MODE == kQ4 && PARTS == 3 ? (D / 16) * NT * 32 * 24 : 0;
@@ -424,6 +426,68 @@ struct Warp {
     }
   }
 
+  // The columns' largest logits of this lane; the maxima raised where one is too far above; weights in the logits' place.
+  static __device__ __forceinline__ void tops(const float (&s)[NT][4], float (&top)[NT][2]) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) top[n][e] = fmaxf(s[n][e], s[n][2 + e]);
+  }
+  __device__ __forceinline__ void raise_to(const float (&top)[NT][2], float c) {
+    bool raise = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) raise |= top[n][e] > limit[n][e];
+    if (!__any_sync(0xffffffffu, raise)) return;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float x = top[n][e];
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+        if (!(x > limit[n][e])) continue;                  // (each column by its own logits alone: roundings too)
+        const float f = x == -INFINITY ? 1.f : ex2((m[n][e] - x) * c);
+        m[n][e] = x;
+        limit[n][e] = x + kRaise / c;
+        sub[n][e] = x == -INFINITY ? 0.f : x * c;
+        l[n][e] *= f;
+#pragma unroll
+        for (int w = 0; w < (MODE == kQ4 ? kGroups : 1); ++w) off[n][e][w] *= f;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) { O[i][n][e] *= f; O[i][n][2 + e] *= f; }
+      }
+  }
+  __device__ __forceinline__ void weigh(float (&s)[NT][4], float c) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        s[n][e] = ex2(fmaf(s[n][e], c, -sub[n][e]));
+        s[n][2 + e] = ex2(fmaf(s[n][2 + e], c, -sub[n][e]));
+        l[n][e] += s[n][e] + s[n][2 + e];
+      }
+  }
+
+  // Two units that every query sees whole, at `at` and `then`: one vote for both, and two chains of products.
+  __device__ __forceinline__ void pair(uint32_t at, uint32_t then, const uint4* shared, float c, int lane) {
+    float s[2][NT][4], top[2][NT][2];
+    logits(at, shared, s[0], lane);
+    logits(then, shared, s[1], lane);
+    tops(s[0], top[0]);
+    tops(s[1], top[1]);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) top[0][n][e] = fmaxf(top[0][n][e], top[1][n][e]);
+    raise_to(top[0], c);
+    weigh(s[0], c);
+    weigh(s[1], c);
+    values<false>(at, s[0], kUnit, lane);
+    values<false>(then, s[1], kUnit, lane);
+  }
+
   // One unit: tokens from `token` on, of which the first `rows` count, in shared memory at `at`.
   __device__ __forceinline__ void unit(uint32_t at, const uint4* shared, int token, int rows, int len, int nq, float c, int lane) {
     const int g = lane >> 2;
@@ -439,43 +503,10 @@ struct Warp {
           if (r >= rows || token + r >= lim[n][e & 1]) s[n][e] = -INFINITY;
         }
     }
-    bool raise = false;
     float top[NT][2];
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        top[n][e] = fmaxf(s[n][e], s[n][2 + e]);
-        raise |= top[n][e] > limit[n][e];
-      }
-    if (__any_sync(0xffffffffu, raise)) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float x = top[n][e];
-#pragma unroll
-          for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-          if (!(x > limit[n][e])) continue;                // (each column by its own logits alone: roundings too)
-          const float f = x == -INFINITY ? 1.f : ex2((m[n][e] - x) * c);
-          m[n][e] = x;
-          limit[n][e] = x + kRaise / c;
-          sub[n][e] = x == -INFINITY ? 0.f : x * c;
-          l[n][e] *= f;
-#pragma unroll
-          for (int w = 0; w < (MODE == kQ4 ? kGroups : 1); ++w) off[n][e][w] *= f;
-#pragma unroll
-          for (int i = 0; i < D / 16; ++i) { O[i][n][e] *= f; O[i][n][2 + e] *= f; }
-        }
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        s[n][e] = ex2(fmaf(s[n][e], c, -sub[n][e]));
-        s[n][2 + e] = ex2(fmaf(s[n][2 + e], c, -sub[n][e]));
-        l[n][e] += s[n][e] + s[n][2 + e];
-      }
+    tops(s, top);
+    raise_to(top, c);
+    weigh(s, c);
     if (!edge) {
       values<false>(at, s, kUnit, lane);
       return;
@@ -583,21 +614,39 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<MODE, D, NT>()) cached_k
     // 4 bits: the queries first, or they would wait behind the ring's first copies, which the arithmetic is behind anyway (two
     // long sequences 45.1 -> 43.4 us).  Rows: the copies first, the cache is all that is waited for (53.3 against 57.3 us).
     if constexpr (MODE == kQ4) take_queries();
+    // (units in pairs where the ring holds two of them and as many again in flight)
+    constexpr bool kPairs = MODE == kQ4 && NT == 1;
+    constexpr int kAhead = kPairs ? S - 2 : S - 1;         // units fetched ahead
 #pragma unroll
-    for (int k = 0; k < S - 1; ++k) fetch(k);
+    for (int k = 0; k < kAhead; ++k) fetch(k);
     if constexpr (MODE != kQ4) take_queries();
     w.clear();
-    int now = 0, next = S - 1, token = first * kUnit;
-    for (int k = 0; k < mine; ++k) {
-      cp_async_wait<S - 2>();
+    int now = 0, next = kAhead, token = first * kUnit;
+    auto after = [](int slot) { return slot + 1 == S ? 0 : slot + 1; };
+    for (int k = 0; k < mine; k += kPairs ? 2 : 1) {
+      cp_async_wait<kPairs ? S - 4 : S - 2>();
       __syncwarp();
       fetch(next);
-      const int rows = (bad >> (S - 1)) & 1 ? 0 : min(kUnit, sg.len - token);
-      w.unit(ring + now * W::kUnitBytes, queries, token, rows, sg.len, a.nq, c, lane);
+      next = after(next);
+      if constexpr (kPairs) {
+        fetch(next);
+        next = after(next);
+        const int then = after(now), last = token + kWarps * kUnit;
+        if (k + 1 < mine && last + kUnit <= sg.len - a.nq + 1 && (bad >> (S - 2) & 3) == 0) {
+          w.pair(ring + now * W::kUnitBytes, ring + then * W::kUnitBytes, queries, c, lane);
+        } else {
+          w.unit(ring + now * W::kUnitBytes, queries, token, bad >> (S - 1) & 1 ? 0 : min(kUnit, sg.len - token), sg.len, a.nq, c, lane);
+          if (k + 1 < mine)
+            w.unit(ring + then * W::kUnitBytes, queries, last, bad >> (S - 2) & 1 ? 0 : min(kUnit, sg.len - last), sg.len, a.nq, c, lane);
+        }
+        token += 2 * kWarps * kUnit;
+        now = after(then);
+      } else {
+        w.unit(ring + now * W::kUnitBytes, queries, token, bad >> (S - 1) & 1 ? 0 : min(kUnit, sg.len - token), sg.len, a.nq, c, lane);
+        token += kWarps * kUnit;
+        now = after(now);
+      }
       __syncwarp();
-      token += kWarps * kUnit;
-      now = now + 1 == S ? 0 : now + 1;
-      next = next + 1 == S ? 0 : next + 1;
     }
     cp_async_wait<0>();
     // ---- the warps' results added: maxima, sums and outputs through shared memory, in the order of the warps
