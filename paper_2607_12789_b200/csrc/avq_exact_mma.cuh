@@ -48,6 +48,11 @@ __device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], 
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_tf32_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {   // from zero
+  asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at));
@@ -86,15 +91,22 @@ __device__ __forceinline__ uint32_t codes_at(uint32_t w, int i) {
   asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(w >> (4 * i)), "r"(0x000f000fu), "r"(0x43004300u));   // (a & b) | c
   return r;
 }
+// c - 8 of such a pair, exactly
+__device__ __forceinline__ uint32_t centred(uint32_t pair) {
+  uint32_t r;
+  asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(pair), "r"(0xc308c308u));   // - 136
+  return r;
+}
 // c 2^-24 of the codes at bits 4 (i - i % 2) of both halves, c 2^-20 of those at bits 4 i (odd i)
 __device__ __forceinline__ uint32_t subnormal_codes(uint32_t w, int i) { return (w >> (8 * (i >> 1))) & ((i & 1) ? 0x00f000f0u : 0x000f000fu); }
 __device__ __forceinline__ float tf32_high(float x) { return __uint_as_float(__float_as_uint(x) & 0xffffe000u); }
-// The low part of a value with the high part h.  An infinity is its own high part; its low part is a number so far below
-// the largest that its products stay finite (those of finite values are smaller still), not a NaN.
-__device__ __forceinline__ float tf32_low(float x, float h) { return fminf(x - h, 1e36f); }
-// The low part of a weight with the high part h, never zero beside one: 2^-30 of it at least, so that an infinite value times
-// it is that infinity and no NaN.
-__device__ __forceinline__ float tf32_low_weight(float p, float h) { return fmaxf(p - h, h * 9.3132257e-10f); }
+// The low part of a value with the high part h, for an operand whose last 13 bits the tensor cores do not read: rounded to
+// the bits that they do.  An infinity is its own high part; its low part is a number so far below the largest that its
+// products stay finite (those of finite values are smaller still), not a NaN.
+__device__ __forceinline__ uint32_t tf32_low(float x, float h) { return __float_as_uint(fminf(x - h, 1e36f)) + 0x1000u; }
+// The same of a weight, never zero beside a high part: 2^-30 of it at least, so that an infinite value times it is that
+// infinity and no NaN.
+__device__ __forceinline__ uint32_t tf32_low_weight(float p, float h) { return __float_as_uint(fmaxf(p - h, h * 9.3132257e-10f)) + 0x1000u; }
 __device__ __forceinline__ float low_f(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float high_f(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
 // Three bfloat16 parts of a pair of float32 values, which add up to them exactly (but for values near the smallest).

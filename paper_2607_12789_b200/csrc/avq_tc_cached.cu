@@ -18,10 +18,12 @@
 //   Keys: a code in the low bits of a 16-bit half is a subnormal number of half precision, c 2^-24, one place further up
 //   c 2^-20; the tensor cores take those exactly, and the queries (brought to 2^14 by a power of two for their row, and
 //   by 2^-4 where the code stands higher) lose nothing that a float32 sum would keep.  An AND makes a pair of codes.
-//   Values: the weights p step_g have a range of their own and stay bfloat16; an AND-OR makes 0x4300 | c, which is 128 + c,
-//   of a code, and a product of the same rounded weights with a constant -128 takes the 128 out again, so that nothing
-//   of a rounding is left behind.
-// float32: rows by tf32 products of two parts each (the lowest product left out: 2^-22 of a term); 4 bits with float32
+//   Values: o_g += (p step_g) (c - 8) + p (lo_g + 8 step_g), the second sum small where values lie about zero, so that the
+//   rounding of the weights meets c - 8 and not c.  The weights p step_g have a range of their own and stay bfloat16; an
+//   AND-OR makes 0x4300 | c, which is 128 + c, of a code, and a product of the same rounded weights with a constant -136
+//   takes the 136 out again.  (With three parts the 136 is taken off the codes: 143 times a part would cost the sum bits.)
+// float32: rows by tf32 products of two parts each (the lowest product left out: 2^-22 of a term; a unit's values are
+// summed from zero and added to the output in registers, since the tensor cores cut sums off); 4 bits with float32
 // queries by three parts of the query (half precision) and of the weight (bfloat16), which are all of their 24 bits.
 //
 // The running maximum of a row is raised only when a logit exceeds it by 2^8 (weights stay below 2^8, sums far inside
@@ -202,7 +204,7 @@ struct Warp {
           const int dim = 16 * (k / 2) + 4 * t + 2 * (k % 2);
           const float x = at(dim), y = at(dim + 1), xh = tf32_high(x), yh = tf32_high(y);
           shared[(k * NT + n) * 32 + lane] =
-              make_uint4(__float_as_uint(xh), __float_as_uint(yh), __float_as_uint(x - xh), __float_as_uint(y - yh));
+              make_uint4(__float_as_uint(xh), __float_as_uint(yh), tf32_low(x, xh), tf32_low(y, yh));
         }
       }
 #pragma unroll
@@ -288,7 +290,7 @@ struct Warp {
           for (int i = 0; i < 4; ++i) {
             const float x = __uint_as_float(hi[i]), h = tf32_high(x);
             hi[i] = __float_as_uint(h);
-            lo[i] = __float_as_uint(x - h);
+            lo[i] = tf32_low(x, h);
           }
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
@@ -336,10 +338,10 @@ struct Warp {
         else lds_words(cw[j], at + kV + r * 32 + (8 * (g >> 1) ^ (16 * ((r >> 2) & 1))));
       }
       const uint32_t half = (g & 1) ? 0x7632u : 0x5410u; // upper or lower halves of two words
-      constexpr uint32_t minus[4] = {0xc300c300u, 0xc300c300u, 0xc300c300u, 0xc300c300u};
+      constexpr uint32_t minus[4] = {0xc308c308u, 0xc308c308u, 0xc308c308u, 0xc308c308u};   // -136
 #pragma unroll
       for (int w = 0; w < kGroups; ++w) {
-        const float sx = high_f(px[w]), sy = high_f(py[w]), lx = low_f(px[w]), ly = low_f(py[w]);
+        const float sx = high_f(px[w]), sy = high_f(py[w]), lx = fmaf(8.f, sx, low_f(px[w])), ly = fmaf(8.f, sy, low_f(py[w]));
         uint32_t b[NT][PARTS][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -371,14 +373,24 @@ struct Warp {
         const uint32_t u = __byte_perm(cw[0][w], cw[1][w], half), v = __byte_perm(cw[2][w], cw[3][w], half);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const uint32_t f[4] = {codes_at(u, 2 * j), codes_at(u, 2 * j + 1), codes_at(v, 2 * j), codes_at(v, 2 * j + 1)};
+          uint32_t f[4] = {codes_at(u, 2 * j), codes_at(u, 2 * j + 1), codes_at(v, 2 * j), codes_at(v, 2 * j + 1)};
+          if constexpr (PARTS == 3) {
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+            for (int i = 0; i < 4; ++i) f[i] = centred(f[i]);
+          }
 #pragma unroll
-            for (int i = PARTS - 1; i >= 0; --i) {
-              mma_bf16(O[2 * w + j][n], f, b[n][i][0], b[n][i][1]);
-              mma_bf16(O[2 * w + j][n], minus, b[n][i][0], b[n][i][1]);
+          for (int n = 0; n < NT; ++n) {
+            if constexpr (PARTS == 3) {
+              float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int i = PARTS - 1; i >= 0; --i) mma_bf16(part, f, b[n][i][0], b[n][i][1]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) O[2 * w + j][n][e] += part[e];
+            } else {
+              mma_bf16(O[2 * w + j][n], f, b[n][0][0], b[n][0][1]);
+              mma_bf16(O[2 * w + j][n], minus, b[n][0][0], b[n][0][1]);
             }
+          }
         }
       }
     } else {
@@ -392,7 +404,7 @@ struct Warp {
           const float x = __shfl_sync(0xffffffffu, p[n][2 * (j >> 1)], from), y = __shfl_sync(0xffffffffu, p[n][2 * (j >> 1) + 1], from);
           const float w = (g & 1) ? y : x, h = tf32_high(w);
           hi[n][j] = __float_as_uint(h);
-          lo[n][j] = __float_as_uint(tf32_low_weight(w, h));
+          lo[n][j] = tf32_low_weight(w, h);
         }
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
@@ -405,23 +417,30 @@ struct Warp {
           v[j][0] = keep ? u.x : 0u; v[j][1] = keep ? u.y : 0u; v[j][2] = keep ? u.z : 0u; v[j][3] = keep ? u.w : 0u;
         }
 #pragma unroll
-        for (int k = 0; k < 2; ++k)                      // tokens 8 k ..
+        for (int i = 0; i < 2; ++i) {
+          float part[NT][4];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
+          for (int k = 0; k < 2; ++k) {                    // tokens 8 k ..
             uint32_t h[4] = {v[2 * k][2 * i], v[2 * k][2 * i + 1], v[2 * k + 1][2 * i], v[2 * k + 1][2 * i + 1]}, x[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float f = __uint_as_float(h[e]), fh = tf32_high(f);
               h[e] = __float_as_uint(fh);
-              x[e] = __float_as_uint(tf32_low(f, fh));
+              x[e] = tf32_low(f, fh);
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-              mma_tf32(O[2 * c + i][n], x, hi[n][2 * k], hi[n][2 * k + 1]);
-              mma_tf32(O[2 * c + i][n], h, lo[n][2 * k], lo[n][2 * k + 1]);
-              mma_tf32(O[2 * c + i][n], h, hi[n][2 * k], hi[n][2 * k + 1]);
+              if (k == 0) mma_tf32_first(part[n], x, hi[n][0], hi[n][1]);
+              else mma_tf32(part[n], x, hi[n][2], hi[n][3]);
+              mma_tf32(part[n], h, lo[n][2 * k], lo[n][2 * k + 1]);
+              mma_tf32(part[n], h, hi[n][2 * k], hi[n][2 * k + 1]);
             }
           }
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) O[2 * c + i][n][e] += part[n][e];
+        }
       }
     }
   }
