@@ -1,13 +1,15 @@
 // Exact attention of packed float32 sequences on the tensor cores (d 64 or 128): every product as three tf32 products of
 // the operands' high and low parts (the product of the two low parts, 2^-22 of a term, is left out), float32 sums.
 //
-// 4 warps, 16 MT rows of one head each, over tiles of 32 keys (of 64, with less of the chip's warps at work: 367 against 339 us
-// for eight images of 785 tokens, 12 heads, d 64).  Queries, keys and values lie in shared memory as they are,
+// 4 warps, 16 MT rows of one head each, over tiles of 32 keys.  Queries, keys and values lie in shared memory as they are,
 // swizzled, and are taken apart in registers: a 16-byte load gives a lane 4 dimensions, which serve as the k indices of two
 // steps of Q K^T (the order of dimensions within a sum is free, as long as both operands have the same) or as the columns
 // of four tiles of P V.  The weights stay in the registers that the logits came in: key 2 t of a tile of 8 is index t of
 // the next product's sum, key 2 t + 1 index t + 4.  The next tile's copies (cp.async) run under the products.
-// Bound by the products, three of each; d = 64: two row tiles to a warp share each key or value taken apart.
+// Bound by the products, three of each, whose sums the tensor cores cut off instead of rounding: the low parts' products have
+// sums of their own in Q K^T, a tile's P V is summed from zero and added in registers (all in one chain: 6.7e-6 of the result
+// off instead of 5.9e-7; only the first of the two left out: 1.1e-6).  Eight images of 785 tokens, 12 heads, d 64: 366 us, of
+// the CUDA cores 540; with one row tile to a warp 367, with three CTAs to an SM, whose registers do not hold the sums, 387.
 #include "avq_exact_mma.cuh"
 
 namespace avq {
@@ -34,7 +36,7 @@ __device__ __forceinline__ void apart(const uint4& x, uint32_t (&hi)[4], uint32_
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) prompt_f32_kernel(const PromptArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArgs a) {
   constexpr int MT = row_tiles<D>(), R = tile_rows<D>(), kChunks = D / 4, kRow = 4 * D;
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ Piece shared_piece;
