@@ -32,7 +32,8 @@ struct CachedArgs {
   const void *Q, *keys, *values;
   void* Y;
   float* lse;
-  float* partial;                // slots of partial results (see Split)
+  float* partial;                // slots of partial results
+  int2* records;                 // of each segment: the first and last CTA that left a part of it, or (-1, ..): one had it all
   const int32_t *table, *lens;
   int64_t q_stride, y_stride;
   int32_t H, Hk, d, B, nq, pages, page, table_pages;
@@ -178,7 +179,8 @@ inline int64_t most_pieces(int64_t T, int64_t S, int64_t rows) { return T / rows
 // block of one key head of one sequence; its tokens are units of kUnit.  The units of all segments, in the order
 // (sequence, key head, block, unit), are dealt out in equal runs to the CTAs, whatever the lengths: a CTA finishes the
 // segments that lie inside its run and leaves partial results of the at most two that do not, its first in slot 2 c,
-// its last in slot 2 c + 1.  join_kernel merges those in the order of the CTAs.
+// its last in slot 2 c + 1.  join_kernel merges those in the order of the CTAs, by the records that the CTAs with the
+// segments' first units leave.
 // A segment also costs a CTA its queries, the start of its copies and the end of its sums, whatever its length: about as much
 // as kSetup units, which stand before its own (six sequences of which one has 4 tokens, float32: 52.6 us
 // without, 41.4 with 8, 30.5 with 16, 29.3 with 32, which costs a step of 64 sequences 2 %).
@@ -226,7 +228,7 @@ struct Place {                   // of the first unit not yet handed out
   int32_t b;
 };
 struct Walk {                    // shared: every thread reads one place and the first writes the next beside it
-  int64_t scratch[34], end;      // end of the CTA's run
+  int64_t scratch[34], end, run; // end of the CTA's run, length of every CTA's
   Place place[2];
 };
 // (64-bit divisions are long; nearly all are of numbers that fit 32 bits.)
@@ -260,7 +262,13 @@ __device__ __forceinline__ bool walk_next(const CachedArgs& a, Walk& w, Segment&
     if (sg.n <= 0) continue;
     sg.b = b; sg.hk = seg / blocks; sg.block = seg % blocks; sg.len = len;
     sg.units = U;
-    if (threadIdx.x == 0) w.place[(turn + 1) & 1] = {at, before, b};
+    if (threadIdx.x == 0) {
+      w.place[(turn + 1) & 1] = {at, before, b};
+      if (sg.unit == 0) {                                  // (the CTA with a segment's first unit tells of it)
+        const int64_t last = before + (int64_t)(seg + 1) * W - 1;
+        a.records[(int64_t)b * per + seg] = sg.n == U ? make_int2(-1, 0) : make_int2(blockIdx.x, (int)quotient(last, w.run));
+      }
+    }
     return true;
   }
   return false;
@@ -303,6 +311,7 @@ __device__ __forceinline__ bool walk_begin(const CachedArgs& a, int least, Walk&
     if (u > 0 && at >= base && at < base + u) {
       w.place[0] = {at, base, b};
       w.end = min(at + run, total);
+      w.run = run;
     }
     before += all;
     if (at < before && blockIdx.x > 0) break;              // (the first CTA looks at every length, to report bad ones)
@@ -326,7 +335,7 @@ avq_status tc_prompt_f32(const PromptArgs& a, cudaStream_t st);
 constexpr int kPromptCtas = 148;                           // (more SMs than that are not asked for)
 size_t tc_prompt_part_bytes(int d);
 avq_status tc_cached(const CachedArgs& a, int dtype, int bits, cudaStream_t st);
-avq_status join(const CachedArgs& a, int dtype, int ctas, int least, cudaStream_t st);
+avq_status join(const CachedArgs& a, int dtype, cudaStream_t st);
 
 }  // namespace exact
 }  // namespace avq

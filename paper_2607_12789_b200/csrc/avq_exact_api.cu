@@ -58,6 +58,11 @@ avq_status validate_cached(const avq_heads* h, int32_t B, int32_t nq) {
   return AVQ_OK;
 }
 
+size_t records_bytes(const avq_heads& h, int32_t B, int32_t nq) {   // a record for each segment, and up to 256 bytes
+  const size_t segments = (size_t)B * h.Hk * (((size_t)nq * (h.H / h.Hk) + kRows - 1) / kRows);
+  return (segments * sizeof(int2) + 255) / 256 * 256;
+}
+
 #define AVQ_TRY(call)                   \
   do {                                  \
     const avq_status s_ = (call);       \
@@ -164,7 +169,7 @@ avq_status avq_cache_read(const avq_cache* cache, const int32_t* slots, int32_t 
 
 size_t avq_cache_attend_workspace_bytes(const avq_heads* heads, int32_t B, int32_t nq) {
   if (validate_cached(heads, B, nq) != AVQ_OK) return 0;
-  return 256 + sizeof(float) * 2 * kMaxCtas * (size_t)slot_floats(heads->d);
+  return 256 + records_bytes(*heads, B, nq) + sizeof(float) * 2 * kMaxCtas * (size_t)slot_floats(heads->d);
 }
 
 avq_status avq_cache_attend(const avq_heads* heads, const avq_cache* cache, const void* Q, int64_t q_stride,
@@ -183,7 +188,8 @@ avq_status avq_cache_attend(const avq_heads* heads, const avq_cache* cache, cons
   AVQ_TRY(validate_rows(Y, y_stride, h.H, h.d, h.dtype));
   if (!workspace || workspace_bytes < avq_cache_attend_workspace_bytes(heads, B, nq)) return AVQ_ERR_WORKSPACE;
   AVQ_TRY(validate_header(workspace));
-  const CachedArgs a = {Q, c.keys, c.values, Y, lse_out, reinterpret_cast<float*>(static_cast<char*>(workspace) + 256),
+  const CachedArgs a = {Q, c.keys, c.values, Y, lse_out, reinterpret_cast<float*>(static_cast<char*>(workspace) + 256 + records_bytes(h, B, nq)),
+                        reinterpret_cast<int2*>(static_cast<char*>(workspace) + 256),
                         table, lens, q_stride, y_stride, h.H, h.Hk, h.d, B, nq, c.pages, c.page, table_pages, h.scale,
                         static_cast<int32_t*>(workspace)};
   cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -356,22 +356,13 @@ __global__ void __launch_bounds__(kCachedThreads) cached_simt_kernel(const Cache
 // ascending order, the warps' sums in the order of the warps.
 constexpr int kJoinThreads = 256;
 template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const CachedArgs a, int ctas, int least) {
-  __shared__ int64_t scratch[33];
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const CachedArgs a) {
   __shared__ float sums[kJoinThreads / 32][256 + 1];
   const int G = a.H / a.Hk, per = segments_per_sequence(a), blocks = per / a.Hk;
   const int b = blockIdx.x / per, seg = blockIdx.x % per;
   const int hk = seg / blocks, block = seg % blocks, r = blockIdx.y;
   const int q = block * kRows + r;
   if (q >= a.nq * G) return;
-  int64_t all = 0, before = 0;
-  for (int i = threadIdx.x; i < a.B; i += kJoinThreads) {
-    const int u = weight_of(units_of(clipped_len(a, i, false)));
-    all += u;
-    if (i < b) before += u;
-  }
-  all = block_sum(all, scratch) * per;
-  before = block_sum(before, scratch) * per;
   const int U = units_of(clipped_len(a, b, false));
   const int64_t token = (int64_t)b * a.nq + q / G;
   const int h = hk * G + q % G, d = a.d;
@@ -381,10 +372,10 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const CachedArgs a, 
     if (a.lse && threadIdx.x == 0) a.lse[token * a.H + h] = -INFINITY;
     return;
   }
-  const int64_t run = run_of(all, ctas, least), g0 = before + (int64_t)seg * weight_of(U) + kSetup;   // the segment's first unit
-  const int c0 = (int)quotient(g0, run), c1 = (int)quotient(g0 + U - 1, run);
-  if (c0 == c1) return;
-  tc::pdl_wait();                                          // the slots come from the kernel before
+  tc::pdl_wait();                                          // records and slots come from the kernel before
+  const int32_t* record = reinterpret_cast<const int32_t*>(a.records + blockIdx.x);
+  const int c0 = tc::ld_after_wait(record), c1 = tc::ld_after_wait(record + 1);
+  if (c0 < 0) return;
   const int64_t size = slot_floats(d);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = c1 - c0 + 1;
   auto slot = [&](int i) { return a.partial + (int64_t)(2 * (c0 + i) + (i == 0)) * size; };
@@ -450,11 +441,11 @@ avq_status simt_prompt(const PromptArgs& a, int dtype, cudaStream_t st) {
        : a.d <= 128 ? launch_prompt<__nv_bfloat16, 128, 8>(a, dev, st) : launch_prompt<__nv_bfloat16, 256, 4>(a, dev, st);
 }
 
-avq_status join(const CachedArgs& a, int dtype, int ctas, int least, cudaStream_t st) {
+avq_status join(const CachedArgs& a, int dtype, cudaStream_t st) {
   const int G = a.H / a.Hk;
   const dim3 grid((unsigned)((int64_t)a.B * a.Hk * ((a.nq * G + kRows - 1) / kRows)), (unsigned)std::min(kRows, a.nq * G));
-  return cuda_ok(dtype == AVQ_F32 ? tc::launch_pdl(join_kernel<float>, grid, dim3(kJoinThreads), 0, st, true, a, ctas, least)
-                                  : tc::launch_pdl(join_kernel<__nv_bfloat16>, grid, dim3(kJoinThreads), 0, st, true, a, ctas, least));
+  return cuda_ok(dtype == AVQ_F32 ? tc::launch_pdl(join_kernel<float>, grid, dim3(kJoinThreads), 0, st, true, a)
+                                  : tc::launch_pdl(join_kernel<__nv_bfloat16>, grid, dim3(kJoinThreads), 0, st, true, a));
 }
 
 namespace {
@@ -467,7 +458,7 @@ avq_status launch_cached(const CachedArgs& a, int dtype, cudaStream_t st) {
   constexpr int ctas = 148 * 2, least = 4;
   cached_simt_kernel<T, BITS><<<ctas, kCachedThreads, cached_smem(a.d), st>>>(a, least);
   s = cuda_ok(cudaGetLastError());
-  return s == AVQ_OK ? join(a, dtype, ctas, least, st) : s;
+  return s == AVQ_OK ? join(a, dtype, st) : s;
 }
 }  // namespace
 

@@ -749,7 +749,7 @@ avq_status launch(const CachedArgs& a, int dtype, cudaStream_t st) {
   const int ctas = min(sms * ctas_per_sm<MODE, D, NT>(), kMaxCtas), least = 2 * kWarps;
   cached_kernel<T, MODE, D, NT><<<ctas, kThreads, cached_smem<MODE, D, NT, PARTS>(), st>>>(a, least);
   s = cuda_ok(cudaGetLastError());
-  return s == AVQ_OK ? join(a, dtype, ctas, least, st) : s;
+  return s == AVQ_OK ? join(a, dtype, st) : s;
 }
 template <typename T, int MODE>
 avq_status launch_rows(const CachedArgs& a, int dtype, cudaStream_t st) {
