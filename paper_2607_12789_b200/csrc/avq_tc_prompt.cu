@@ -17,6 +17,9 @@
 // exponentials as many of the MUFU pipe, in turn for each tile of rows; what keeps them from overlapping fully is the way
 // from logits to weights and back.  A quarter of the exponentials by a polynomial on the FMA pipe was 4 % slower than
 // none (16384 tokens of 16 heads: 949 and 906 us): a second form of the code costs more than the pipe gains.
+// Measured: 16384 tokens, 16 heads on 4, d 128, causal 868 us (1267 TFLOP/s, 76 % of the measured burst rate; 1047 us and 1050
+// TFLOP/s when it runs on and on at the power limit), 16 prompts of up to 2048 tokens, 32 heads on 8, 182 us (710 TFLOP/s: a third
+// of the time is the first logits and the outputs of each of 1704 short pieces), d 64 620 TFLOP/s (bound by the exponentials).
 // The maximum that weights refer to is raised only when a row exceeds it by 2^8, which spares nearly every rescaling of
 // O: weights stay below 2^8, and what they are relative to cancels in O / l.
 #include "avq_exact.cuh"
