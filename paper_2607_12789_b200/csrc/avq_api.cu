@@ -321,7 +321,7 @@ const char* avq_status_string(avq_status s) {
     case AVQ_ERR_WORKSPACE: return "workspace is NULL or too small";
     case AVQ_ERR_CUDA: return "a CUDA call failed";
     case AVQ_ERR_DEVICE_TIMEOUT: return "a bounded device-side wait expired";
-    case AVQ_ERR_INDEX: return "a parent or child index read by a kernel was out of range";
+    case AVQ_ERR_INDEX: return "an index, bound or length read by a kernel was out of range";
   }
   return "unknown status";
 }

@@ -102,7 +102,7 @@ avq_status avq_prompt_attend(const avq_heads* heads, const void* Q, int64_t q_st
   }
   if (!workspace || workspace_bytes < 256) return AVQ_ERR_WORKSPACE;
   AVQ_TRY(validate_header(workspace));
-  if (S > (1 << 20)) return AVQ_ERR_UNSUPPORTED;
+  if (S > (1 << 16)) return AVQ_ERR_UNSUPPORTED;         // (every CTA passes over the sequences behind its own)
   const PromptArgs a = {Q, K, V, Y, lse_out, cu_q, cu_k, q_stride, k_stride, v_stride, y_stride, h.H, h.Hk, h.d, S, Tq, Tk,
                         (h.flags & AVQ_FLAG_CAUSAL) ? 1 : 0, h.scale, static_cast<int32_t*>(workspace),
                         workspace_bytes > 256 && workspace_bytes >= avq_prompt_split_bytes(heads)

@@ -356,27 +356,31 @@ __global__ void __launch_bounds__(kCachedThreads) cached_simt_kernel(const Cache
 // One CTA per row of a segment: nothing to do if one CTA held the whole segment; zeros if the sequence is empty;
 // otherwise the partial rows of CTAs c0 .. c1 are brought to their common maximum and added, each warp a share of them in
 // ascending order, the warps' sums in the order of the warps.
-constexpr int kJoinThreads = 256;
+// Threads of a row's CTA: two warps where segments are many (and parts of each few), eight where they are few (their parts
+// many).  64 and 256 threads: 512 segments 78.9 and 84.9 us with the kernel before, 24 segments 31.8 and 30.5, 8 segments 43.5
+// and 38.9.
+constexpr int kJoinMost = 256, kJoinFew = 64, kJoinMany = 128;
 template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const CachedArgs a) {
-  __shared__ float sums[kJoinThreads / 32][256 + 1];
+__global__ void __launch_bounds__(kJoinMost) join_kernel(const CachedArgs a) {
+  const int threads = blockDim.x, warps = threads >> 5;
+  __shared__ float sums[kJoinMost / 32][256 + 1];
+  tc::pdl_wait();                                          // records and slots come from the kernel before
   const int G = a.H / a.Hk, per = segments_per_sequence(a), blocks = per / a.Hk;
   const int b = blockIdx.x / per, seg = blockIdx.x % per;
   const int hk = seg / blocks, block = seg % blocks, r = blockIdx.y;
   const int q = block * kRows + r;
   if (q >= a.nq * G) return;
+  const int32_t* record = reinterpret_cast<const int32_t*>(a.records + blockIdx.x);
+  const int c0 = tc::ld_after_wait(record), c1 = tc::ld_after_wait(record + 1);   // (of an empty sequence: anything)
   const int U = units_of(clipped_len(a, b, false));
   const int64_t token = (int64_t)b * a.nq + q / G;
   const int h = hk * G + q % G, d = a.d;
   T* Y = static_cast<T*>(a.Y) + token * a.y_stride + (int64_t)h * d;
   if (U == 0) {
-    for (int c = threadIdx.x; c < d; c += kJoinThreads) Y[c] = from_f32<T>(0.f);
+    for (int c = threadIdx.x; c < d; c += threads) Y[c] = from_f32<T>(0.f);
     if (a.lse && threadIdx.x == 0) a.lse[token * a.H + h] = -INFINITY;
     return;
   }
-  tc::pdl_wait();                                          // records and slots come from the kernel before
-  const int32_t* record = reinterpret_cast<const int32_t*>(a.records + blockIdx.x);
-  const int c0 = tc::ld_after_wait(record), c1 = tc::ld_after_wait(record + 1);
   if (c0 < 0) return;
   const int64_t size = slot_floats(d);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = c1 - c0 + 1;
@@ -389,11 +393,11 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const CachedArgs a) 
   float l = 0.f, x[8] = {};                                // columns lane + 32 j
   // a batch of partial rows per turn, all its loads in flight together
   constexpr int kBatch = 4;
-  for (int i0 = warp; i0 < n; i0 += kBatch * (kJoinThreads / 32)) {
+  for (int i0 = warp; i0 < n; i0 += kBatch * warps) {
     float top[kBatch], sum[kBatch], part[kBatch][8];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-      const int i = i0 + k * (kJoinThreads / 32);
+      const int i = i0 + k * warps;
       top[k] = -INFINITY;
       sum[k] = 0.f;
       if (i >= n) continue;
@@ -419,13 +423,11 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const CachedArgs a) 
   if (lane == 0) sums[warp][256] = l;
   __syncthreads();
   l = 0.f;
-#pragma unroll
-  for (int w = 0; w < kJoinThreads / 32; ++w) l += sums[w][256];
+  for (int w = 0; w < warps; ++w) l += sums[w][256];
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  for (int c = threadIdx.x; c < d; c += kJoinThreads) {
+  for (int c = threadIdx.x; c < d; c += threads) {
     float y = 0.f;
-#pragma unroll
-    for (int w = 0; w < kJoinThreads / 32; ++w) y += sums[w][c];
+    for (int w = 0; w < warps; ++w) y += sums[w][c];
     Y[c] = from_f32<T>(y * inv);
   }
   if (a.lse && threadIdx.x == 0) a.lse[token * a.H + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
@@ -446,8 +448,9 @@ avq_status simt_prompt(const PromptArgs& a, int dtype, cudaStream_t st) {
 avq_status join(const CachedArgs& a, int dtype, cudaStream_t st) {
   const int G = a.H / a.Hk;
   const dim3 grid((unsigned)((int64_t)a.B * a.Hk * ((a.nq * G + kRows - 1) / kRows)), (unsigned)std::min(kRows, a.nq * G));
-  return cuda_ok(dtype == AVQ_F32 ? tc::launch_pdl(join_kernel<float>, grid, dim3(kJoinThreads), 0, st, true, a)
-                                  : tc::launch_pdl(join_kernel<__nv_bfloat16>, grid, dim3(kJoinThreads), 0, st, true, a));
+  const dim3 block(grid.x >= kJoinMany ? kJoinFew : kJoinMost);
+  return cuda_ok(dtype == AVQ_F32 ? tc::launch_pdl(join_kernel<float>, grid, block, 0, st, true, a)
+                                  : tc::launch_pdl(join_kernel<__nv_bfloat16>, grid, block, 0, st, true, a));
 }
 
 namespace {

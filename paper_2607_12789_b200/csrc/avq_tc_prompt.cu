@@ -671,6 +671,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) prompt_join_kernel(const Prom
   __shared__ int32_t before[kMostSplit + 1];
   __shared__ Piece shared_piece;
   __shared__ int found;
+  pdl_wait();                                              // (every CTA: the grid's end is to mean the end of the kernel before, too)
   const int G = a.H / a.Hk, per = kTile / G, k = blockIdx.x / a.Hk, hk = blockIdx.x % a.Hk;
   if (threadIdx.x < 32) {
     sum_tiles(a, per, pieces, bounds, before);
@@ -688,7 +689,6 @@ __global__ void __launch_bounds__(32 * kJoinWarps) prompt_join_kernel(const Prom
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int r = blockIdx.y * kJoinRows + lane, i = r / kTile, x = r % kTile, token = pc.first + i * per + x / G;
   if (x >= per * G || token >= pc.nq) return;
-  pdl_wait();                                              // the parts come from the kernel before
   constexpr int kPer = D / kJoinWarps, kBatch = 4;         // columns of a lane, parts in flight together
   const int n = U > 0 ? c1 - c0 + 1 : 0;
   auto slot = [&](int p) { return parts + (int64_t)(2 * (c0 + p) + (p == 0)) * part_floats(D); };

@@ -143,6 +143,27 @@ def test_prompt_rows_as_views_and_on_another_stream(dtype, flags):
     assert torch.equal(big[:, 1:1 + H], want) and (big[:, 0] == 9).all() and (big[:, -1] == 9).all()
 
 
+@pytest.mark.parametrize("dtype,flags,d", [(F32, 0, 64), (F32, 0, 128), (F32, 0, 40), (BF16, SIMT, 64), (BF16, 0, 64), (BF16, 0, 128)])
+def test_no_keys_at_all_and_rows_aligned_to_16_bytes_only(dtype, flags, d):
+    """Without any key every row is zero and every sum -inf; rows 16 bytes further apart than they are long give the same."""
+    g = _gen(27)
+    H, Hk, n = 4, 2, 37
+    att = binding.ExactAttention(H, Hk, d, dtype=dtype, flags=flags)
+    Q = _randn(g, n, H, d, dtype=dtype)
+    none = Q[:0, :Hk]
+    Y, L = att(Q, none, none, _ints([0, 20, n]), _ints([0, 0, 0]), lse=True)
+    att.check()
+    assert (Y == 0).all() and torch.isinf(L).all() and (L < 0).all()
+    more = 16 // Q.element_size()
+    apart = lambda t: torch.zeros(n * (t.shape[1] * d + more), dtype=dtype, device="cuda").as_strided(
+        t.shape, (t.shape[1] * d + more, d, 1)).copy_(t)
+    K, V = _randn(g, n, Hk, d, dtype=dtype), _randn(g, n, Hk, d, dtype=dtype)
+    want = att(Q, K, V, _ints([0, 20, n]))
+    Y = apart(torch.zeros_like(Q))
+    att(apart(Q), apart(K), apart(V), _ints([0, 20, n]), Y=Y)
+    assert torch.equal(Y, want)
+
+
 @pytest.mark.parametrize("dtype,flags", [(F32, 0), (BF16, SIMT), (BF16, 0)])
 def test_unusable_bounds_are_left_out_and_reported(dtype, flags):
     g = _gen(29)
