@@ -220,7 +220,7 @@ avq_status launch_prompt(const PromptArgs& a, int dev, cudaStream_t st) {
 // A CTA walks its run of units (avq_exact.cuh), 32 tokens of a segment at a time: their keys and values go to shared
 // memory as float32, every (row, token) pair's logit is one thread's, weights and running maxima are a warp's per row,
 // and a thread owns output columns.  The kernel for the shapes that no other takes: 64 sequences over a bfloat16 cache at
-// d 128 1454 us, where the tensor-core kernel takes 85.
+// d 128 1454 us, where the tensor-core kernel takes 78.5.
 constexpr int kCachedThreads = 128, kCachedTokens = 32;
 inline size_t cached_smem(int d) {
   return sizeof(float) * ((size_t)kRows * d + (size_t)kCachedTokens * (2 * d + 4) + kRows * kCachedTokens + 3 * kRows);
