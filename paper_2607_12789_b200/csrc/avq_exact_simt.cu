@@ -336,7 +336,8 @@ __global__ void __launch_bounds__(kCachedThreads) cached_simt_kernel(const Cache
       for (int k = 0; k < kRows; ++k)                      // (a register array has no run-time index)
         if (k == r) { o[0] = O[k][0]; o[1] = O[k][1]; }
       if (slot) {
-        if (tid == 0) { slot[r] = ms[r]; slot[kRows + r] = ls[r]; }
+        // (a share that met nothing but NaN has raised no maximum: it must not pass for one that saw no token)
+        if (tid == 0) { slot[r] = ls[r] == ls[r] ? ms[r] : ls[r]; slot[kRows + r] = ls[r]; }
       } else if (a.lse && tid == 0) {
         a.lse[token * a.H + h] = ls[r] == 0.f ? -INFINITY : (ms[r] + log2f(ls[r])) * kLn2;
       }

@@ -685,6 +685,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<MODE, D, NT>()) cached_k
           for (int x = 0; x < (MODE == kQ4 ? W::kGroups : 1); ++x)
             if (MODE == kQ4) w.off[n][e][x] += __shfl_xor_sync(0xffffffffu, w.off[n][e][x], o);
         }
+        // (a warp that met nothing but NaN has raised no maximum: it must not pass for one that saw no token)
+        if (w.l[n][e] != w.l[n][e]) w.m[n][e] = w.l[n][e];
         if (g == 0) { ms[warp][8 * n + 2 * t + e] = w.m[n][e]; ls[warp][8 * n + 2 * t + e] = w.l[n][e]; }
       }
     __syncthreads();                                       // (every warp is done with its ring: it holds the outputs now)
@@ -728,7 +730,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<MODE, D, NT>()) cached_k
 #pragma unroll
         for (int i = 0; i < kPer; ++i) y[i] += out[(x * 8 * NT + r) * kPitch + kPer * lane + i];
       if (slot) {
-        if (lane == 0) { slot[r] = top == -INFINITY ? -INFINITY : top * c; slot[kRows + r] = sum; }
+        if (lane == 0) { slot[r] = sum != sum ? sum : top == -INFINITY ? -INFINITY : top * c; slot[kRows + r] = sum; }
 #pragma unroll
         for (int i = 0; i < kPer; ++i) slot[2 * kRows + r * D + kPer * lane + i] = y[i];
       } else {

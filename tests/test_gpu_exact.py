@@ -485,6 +485,54 @@ def test_a_later_token_has_no_effect_on_an_earlier_query(dtype, bits, flags, bad
 
 @pytest.mark.parametrize("dtype,bits", TYPES, ids=IDS)
 @pytest.mark.parametrize("flags", [SIMT, 0], ids=["simt", "tc"])
+@pytest.mark.parametrize("d,nq,lens", [(64, 1, [1, 20, 0, 333]), (128, 3, [70, 3, 500]), (64, 1, [9000]), (128, 2, [6000, 40])])
+def test_nan_in_queries_and_whole_units_of_tokens_stays_nan(dtype, bits, flags, d, nq, lens):
+    """Rows whose logits are all NaN, in the whole sequence or in what one warp or CTA has of it, are NaN; others are as before."""
+    g = _gen(67)
+    H, Hk, B = 4, 2, len(lens)
+    c = _cache(sum(-(-n // 16) for n in lens) + 2, 16, Hk, d, dtype, bits, g)
+    Q, table = _cached(c, H, lens, nq, flags, g)
+    plan = c.plan(H, B, nq, flags=flags)
+    Y, L = c.attend(Q, table, _ints(lens), lse=True, plan=plan)
+    for b, n in enumerate(lens):
+        if not n:
+            continue
+        row, Q2 = b * nq + nq - 1, Q.clone()
+        Q2[row, 1] = math.nan                                # one head of the sequence's newest query
+        Y2, L2 = c.attend(Q2, table, _ints(lens), lse=True, plan=plan)
+        assert torch.isnan(Y2[row, 1].float()).all() and torch.isnan(L2[row, 1])
+        Y2[row, 1], L2[row, 1] = Y[row, 1], L[row, 1]
+        assert torch.equal(Y2, Y) and torch.equal(L2, L)
+    b = B - 1                                               # 16 tokens of NaN keys in front, which every query sees
+    slots = table[b, 0] * 16 + torch.arange(16, dtype=torch.int32, device="cuda")
+    x = torch.full((16, Hk, d), math.nan, dtype=dtype, device="cuda")
+    c.append(x, torch.zeros_like(x), slots)
+    Y2, L2 = c.attend(Q, table, _ints(lens), lse=True, plan=plan)
+    assert torch.isnan(Y2[b * nq:].float()).all() and torch.isnan(L2[b * nq:]).all()
+    assert torch.equal(Y2[:b * nq], Y[:b * nq]) and torch.equal(L2[:b * nq], L[:b * nq])
+    c.check(plan)
+
+
+@pytest.mark.parametrize("dtype,flags,d", [(F32, 0, 64), (F32, SIMT, 96), (BF16, SIMT, 64), (BF16, 0, 64), (BF16, 0, 128)])
+@pytest.mark.parametrize("lq,lk", [([1, 40, 200], [1, 40, 200]), ([20, 3], [3000, 2500])])
+def test_a_nan_query_gives_a_nan_row(dtype, flags, d, lq, lk):
+    g = _gen(68)
+    H, Hk, cq = 4, 2, _ends(lq)
+    Q, K, V = (_randn(g, n, m, d, dtype=dtype) for n, m in ((sum(lq), H), (sum(lk), Hk), (sum(lk), Hk)))
+    att = binding.ExactAttention(H, Hk, d, dtype=dtype, flags=flags)
+    Y, L = att(Q, K, V, _ints(cq), _ints(_ends(lk)), lse=True)
+    for row in [cq[s + 1] - 1 for s in range(len(lq))]:
+        Q2 = Q.clone()
+        Q2[row, 2] = math.nan
+        Y2, L2 = att(Q2, K, V, _ints(cq), _ints(_ends(lk)), lse=True)
+        assert torch.isnan(Y2[row, 2].float()).all() and torch.isnan(L2[row, 2])
+        Y2[row, 2], L2[row, 2] = Y[row, 2], L[row, 2]
+        assert torch.equal(Y2, Y) and torch.equal(L2, L)
+    att.check()
+
+
+@pytest.mark.parametrize("dtype,bits", TYPES, ids=IDS)
+@pytest.mark.parametrize("flags", [SIMT, 0], ids=["simt", "tc"])
 def test_unusable_pages_and_lengths_are_left_out_and_reported(dtype, bits, flags):
     g = _gen(61)
     c = _cache(12, 16, 1, 64, dtype, bits, g)
