@@ -299,7 +299,8 @@ typedef struct {
  *   Tensor-core kernels: d in {64, 128}, scale > 0; avq_prompt_attend in bfloat16: H / Hk <= 128.
  *   avq_prompt_attend in float32 takes what the CUDA cores take without the flag too, and runs d in {64, 128} on the tensor
  *   cores, to the same precision (three products of the operands' high and low parts).
- *   Prompts: S <= 65536.  Caches: page a multiple of 16, 16..1024; pages * page < 2^31; in 4 bits d % 32 == 0.
+ *   Rows of a call and tokens of a sequence (Tq, Tk, T, table_pages * page) below 2^30.  Prompts: S <= 65536.  Caches: page a
+ *   multiple of 16, 16..1024; pages * page < 2^31; in 4 bits d % 32 == 0.
  *   Sums are float32 of weights up to 2^8 (the running reference of a row's weights is raised only beyond that): values
  *   up to 2^100 in magnitude keep them finite.
  */

@@ -27,6 +27,8 @@ avq_status validate_heads(const avq_heads* h) {
   if (h->d % 8 != 0 || h->d > 256 || h->H > 65535) return AVQ_ERR_UNSUPPORTED;
   return AVQ_OK;
 }
+// Rows of a call, tokens of a sequence: beyond, sums of row numbers and tiles would pass 32 bits.
+bool too_many(int64_t rows) { return rows >= (int64_t)1 << 30; }
 size_t es(int dtype) { return dtype == AVQ_F32 ? 4 : 2; }
 // Rows of n heads, `stride` elements apart.
 avq_status validate_rows(const void* p, int64_t stride, int64_t n, int d, int dtype) {
@@ -102,6 +104,7 @@ avq_status avq_prompt_attend(const avq_heads* heads, const void* Q, int64_t q_st
   }
   if (!workspace || workspace_bytes < 256) return AVQ_ERR_WORKSPACE;
   AVQ_TRY(validate_header(workspace));
+  if (too_many(Tq) || too_many(Tk)) return AVQ_ERR_UNSUPPORTED;
   if (S > (1 << 16)) return AVQ_ERR_UNSUPPORTED;         // (every CTA passes over the sequences behind its own)
   const PromptArgs a = {Q, K, V, Y, lse_out, cu_q, cu_k, q_stride, k_stride, v_stride, y_stride, h.H, h.Hk, h.d, S, Tq, Tk,
                         (h.flags & AVQ_FLAG_CAUSAL) ? 1 : 0, h.scale, static_cast<int32_t*>(workspace),
@@ -146,7 +149,7 @@ avq_status avq_cache_append(const avq_cache* cache, const void* K, int64_t k_str
                         turn ? rot->pos : nullptr, k_stride, v_stride, q_stride, q_out_stride, T,
                         Q ? H : 0, c.Hk, c.d, c.page, c.pages, turn ? rot->rows : 0, turn ? rot->dims : 0,
                         turn ? rot->adjacent : 0, static_cast<int32_t*>(header)};
-  if ((int64_t)T * heads >= (int64_t)1 << 34) return AVQ_ERR_UNSUPPORTED;
+  if (too_many(T) || (int64_t)T * heads >= (int64_t)1 << 34) return AVQ_ERR_UNSUPPORTED;
   return cache_append(a, c.dtype, c.bits, static_cast<cudaStream_t>(stream));
 }
 
@@ -163,7 +166,7 @@ avq_status avq_cache_read(const avq_cache* cache, const int32_t* slots, int32_t 
   AVQ_TRY(validate_header(header));
   const ReadArgs a = {c.keys, c.values, K, V, slots, k_stride, v_stride, T, c.Hk, c.d, c.page, c.pages,
                       static_cast<int32_t*>(header)};
-  if ((int64_t)T * 2 * c.Hk >= (int64_t)1 << 34) return AVQ_ERR_UNSUPPORTED;
+  if (too_many(T) || (int64_t)T * 2 * c.Hk >= (int64_t)1 << 34) return AVQ_ERR_UNSUPPORTED;
   return cache_read(a, c.dtype, c.bits, static_cast<cudaStream_t>(stream));
 }
 
@@ -180,7 +183,7 @@ avq_status avq_cache_attend(const avq_heads* heads, const avq_cache* cache, cons
   const avq_heads& h = *heads;
   const avq_cache& c = *cache;
   if (c.Hk != h.Hk || c.d != h.d || c.dtype != h.dtype || table_pages < 0) return AVQ_ERR_SHAPE;
-  if ((int64_t)table_pages * c.page >= (int64_t)1 << 31) return AVQ_ERR_UNSUPPORTED;
+  if (too_many((int64_t)table_pages * c.page)) return AVQ_ERR_UNSUPPORTED;
   if (B == 0) return AVQ_OK;
   if (!c.keys || !c.values || !lens || (table_pages > 0 && !table)) return AVQ_ERR_NULL;
   if (!aligned16(c.keys) || !aligned16(c.values)) return AVQ_ERR_ALIGN;

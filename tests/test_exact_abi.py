@@ -99,6 +99,18 @@ def test_unusable_rows_are_refused(lib):
     assert get(sl=0) == 1 and get(K=0) == 1 and get(vs=120) == 2 and get(V=ODD) == 4 and get(T=-1) == 2
 
 
+def test_numbers_of_rows_that_pass_32_bits_in_sums_are_refused(lib):
+    many = 1 << 30
+    one = _heads(H=1, Hk=1)
+    assert _prompt(lib, one, Tq=many) == 3 and _prompt(lib, one, Tk=many) == 3 and _prompt(lib, one, ck=0, Tq=2 ** 31 - 1, Tk=2 ** 31 - 1) == 3
+    c = _cache(Hk=1)
+    for T in (many, 2 ** 31 - 1):
+        assert lib.avq_cache_append(c, OK, 64, OK, 64, OK, T, None, 0, 0, 0, 0, 0, 0, 0) == 3
+        assert lib.avq_cache_read(c, OK, T, OK, 64, OK, 64, 0, 0) == 3
+    n = lib.avq_cache_attend_workspace_bytes(one, 1, 1)
+    assert lib.avq_cache_attend(one, c, OK, 64, OK, many // 16, OK, 1, 1, OK, 64, 0, OK, n, 0) == 3
+
+
 def test_unusable_cached_calls_are_refused(lib):
     n = lib.avq_cache_attend_workspace_bytes(_heads(), 3, 1)
     assert n > 256
