@@ -28,8 +28,9 @@
 //
 // Measured (B200, several calls one after another): 64 sequences of 1 .. 4096 tokens, 8 key heads, d 128, bfloat16 rows 78.5 us
 // for 467 MB, 5.95 TB/s, 91 % of the measured copy rate, the joining kernel in it; the same in 4 bits, lengths to 8192, with the
-// rows' way into the cache 91.7 us for 268 MB (2.9 TB/s) and two sequences of 131072 and 28076 39 us for 102 MB: there the instructions that take codes apart and scale
-// (450 for 16 tokens of one head, half of the issue slots) and the start of the CTAs are the time; float32 rows 30 us for 105 MB.
+// rows' way into the cache 91.7 us for 268 MB (2.9 TB/s), two sequences of 131072 and 28076 39 us for 102 MB: there the
+// instructions that take codes apart and scale (450 for 16 tokens of one head, half of the issue slots) and the start of the
+// CTAs are the time; float32 rows 31 us for 105 MB.
 //
 // The running maximum of a row is raised only when a logit exceeds it by 2^8 (weights stay below 2^8, sums far inside
 // float32): most units need a vote instead of shuffles and rescaling.
