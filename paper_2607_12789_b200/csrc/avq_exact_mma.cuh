@@ -99,10 +99,16 @@ __device__ __forceinline__ uint32_t centred(uint32_t pair) {
 }
 // c 2^-24 of the codes at bits 4 (i - i % 2) of both halves, c 2^-20 of those at bits 4 i (odd i)
 __device__ __forceinline__ uint32_t subnormal_codes(uint32_t w, int i) { return (w >> (8 * (i >> 1))) & ((i & 1) ? 0x00f000f0u : 0x000f000fu); }
+__device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 __device__ __forceinline__ float tf32_high(float x) { return __uint_as_float(__float_as_uint(x) & 0xffffe000u); }
 // The low part of a value with the high part h, for an operand whose last 13 bits the tensor cores do not read: rounded to
-// the bits that they do.  An infinity is its own high part; its low part is a number so far below the largest that its
-// products stay finite (those of finite values are smaller still), not a NaN.
+// the bits that they do.  An infinity is its own high part; its low part is a number far above those of finite values, not a
+// NaN.  (The product of an infinity and a low part of zero is NaN all the same, and that of the number and a factor above 340
+// is an infinity of the other sign, perhaps: logits that are NaN are taken again from the operands themselves.)
 __device__ __forceinline__ uint32_t tf32_low(float x, float h) { return __float_as_uint(fminf(x - h, 1e36f)) + 0x1000u; }
 // The same of a weight, never zero beside a high part: 2^-30 of it at least, so that an infinite value times it is that
 // infinity and no NaN.

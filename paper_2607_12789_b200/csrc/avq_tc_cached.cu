@@ -310,6 +310,31 @@ struct Warp {
     }
   }
 
+  // (float32 rows) The parts of an infinity can make a NaN of a logit that is none: such logits once more, from the rows
+  // themselves.  (A row that has had a NaN keeps it.)
+  __device__ __forceinline__ void mend_logits(uint32_t at, const CachedArgs& a, const Segment& sg, float (&s)[NT][4], int lane) {
+    const int g = lane >> 2, t = lane & 3, G = a.H / a.Hk, rows = min(kRows, a.nq * G - sg.block * kRows);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int c = 8 * n + 2 * t + (e & 1), r = g + 8 * (e >> 1), q = sg.block * kRows + c;
+        if (s[n][e] == s[n][e] || l[n][e & 1] != l[n][e & 1] || c >= rows) continue;
+        const float* src = static_cast<const float*>(a.Q) + ((int64_t)sg.b * a.nq + q / G) * a.q_stride + ((int64_t)sg.hk * G + q % G) * D;
+        float sum = 0.f;
+#pragma unroll 1
+        for (int k = 0; k < D / 4; ++k) {
+          const float4 x = reinterpret_cast<const float4*>(src)[k];
+          const uint4 y = lds128(at + r * (4 * D) + 16 * (k ^ swizzle(r)));
+          sum = fmaf(x.x, __uint_as_float(y.x), sum);
+          sum = fmaf(x.y, __uint_as_float(y.y), sum);
+          sum = fmaf(x.z, __uint_as_float(y.z), sum);
+          sum = fmaf(x.w, __uint_as_float(y.w), sum);
+        }
+        s[n][e] = sum;
+      }
+  }
+
   // O^T += V^T P^T for one unit.  p: weights in the layout of the logits.
   // SKIP: tokens from `seen` on do not exist for this product (raw rows: their values are made zero).
   template <bool SKIP>
@@ -514,8 +539,9 @@ struct Warp {
   }
 
   // One unit: tokens from `token` on, of which the first `rows` count, in shared memory at `at`.
-  __device__ __forceinline__ void unit(uint32_t at, const uint4* shared, int token, int rows, int len, int nq, float c, int lane) {
-    const int g = lane >> 2;
+  __device__ __forceinline__ void unit(uint32_t at, const uint4* shared, const CachedArgs& a, const Segment& sg, int token, int rows, float c,
+                                       int lane) {
+    const int g = lane >> 2, len = sg.len, nq = a.nq;
     float s[NT][4];
     logits(at, shared, s, lane);
     const bool edge = rows < kUnit || token + kUnit > len - nq + 1;
@@ -527,6 +553,14 @@ struct Warp {
           const int r = g + 8 * (e >> 1);
           if (r >= rows || token + r >= lim[n][e & 1]) s[n][e] = -INFINITY;
         }
+    }
+    if constexpr (MODE == kF32) {
+      float all = s[0][0];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) all = max_nan(all, s[n][e]);
+      if (all != all) mend_logits(at, a, sg, s, lane);
     }
     float top[NT][2];
     tops(s, top);
@@ -660,14 +694,14 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<MODE, D, NT>()) cached_k
         if (k + 1 < mine && last + kUnit <= sg.len - a.nq + 1 && (bad >> (S - 2) & 3) == 0) {
           w.pair(ring + now * W::kUnitBytes, ring + then * W::kUnitBytes, queries, c, lane);
         } else {
-          w.unit(ring + now * W::kUnitBytes, queries, token, bad >> (S - 1) & 1 ? 0 : min(kUnit, sg.len - token), sg.len, a.nq, c, lane);
+          w.unit(ring + now * W::kUnitBytes, queries, a, sg, token, bad >> (S - 1) & 1 ? 0 : min(kUnit, sg.len - token), c, lane);
           if (k + 1 < mine)
-            w.unit(ring + then * W::kUnitBytes, queries, last, bad >> (S - 2) & 1 ? 0 : min(kUnit, sg.len - last), sg.len, a.nq, c, lane);
+            w.unit(ring + then * W::kUnitBytes, queries, a, sg, last, bad >> (S - 2) & 1 ? 0 : min(kUnit, sg.len - last), c, lane);
         }
         token += 2 * kWarps * kUnit;
         now = after(then);
       } else {
-        w.unit(ring + now * W::kUnitBytes, queries, token, bad >> (S - 1) & 1 ? 0 : min(kUnit, sg.len - token), sg.len, a.nq, c, lane);
+        w.unit(ring + now * W::kUnitBytes, queries, a, sg, token, bad >> (S - 1) & 1 ? 0 : min(kUnit, sg.len - token), c, lane);
         token += kWarps * kUnit;
         now = after(now);
       }

@@ -35,6 +35,21 @@ __device__ __forceinline__ void apart(const uint4& x, uint32_t (&hi)[4], uint32_
   }
 }
 
+// The product of rows qr and kr as they lie in shared memory, in float32.
+template <int D>
+__device__ __forceinline__ float plain_product(uint32_t qs, int qr, uint32_t kt, int kr) {
+  float s = 0.f;
+#pragma unroll 1
+  for (int c = 0; c < D / 4; ++c) {
+    const uint4 x = lds128(qs + qr * 4 * D + 16 * (c ^ swizzle(qr))), y = lds128(kt + kr * 4 * D + 16 * (c ^ swizzle(kr)));
+    s = fmaf(__uint_as_float(x.x), __uint_as_float(y.x), s);
+    s = fmaf(__uint_as_float(x.y), __uint_as_float(y.y), s);
+    s = fmaf(__uint_as_float(x.z), __uint_as_float(y.z), s);
+    s = fmaf(__uint_as_float(x.w), __uint_as_float(y.w), s);
+  }
+  return s;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArgs a) {
   constexpr int MT = row_tiles<D>(), R = tile_rows<D>(), kChunks = D / 4, kRow = 4 * D;
@@ -131,12 +146,13 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArg
     }
     const int k0 = j * kKeys;
     const bool edge = k0 + kKeys > pc.nk || (a.causal && k0 + kKeys > shift + 1);
+    float tops[MT][2], all = -INFINITY;                    // NaN if any logit of the row, of this lane is
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int row = 16 * (MT * warp + i) + g + 8 * x;
-        float top = -INFINITY;
+        tops[i][x] = -INFINITY;
 #pragma unroll
         for (int n = 0; n < kKeys / 8; ++n)
 #pragma unroll
@@ -147,8 +163,34 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArg
               const int key = k0 + 8 * n + 2 * t + e;
               if (key >= pc.nk || (a.causal && key > row + shift)) v = -INFINITY;
             }
-            top = fmaxf(top, v);
+            tops[i][x] = max_nan(tops[i][x], v);
           }
+        all = max_nan(all, tops[i][x]);
+      }
+    if (all != all) {
+      // The parts of an infinity can make a NaN of a logit that is none: such logits once more, from the rows themselves.
+      // (A row that has had a NaN keeps it.)
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          tops[i][x] = -INFINITY;
+#pragma unroll
+          for (int n = 0; n < kKeys / 8; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float& v = s[i][n][2 * x + e];
+              if (v != v && l[i][x] == l[i][x])
+                v = plain_product<D>(qs, 16 * (MT * warp + i) + g + 8 * x, kt, 8 * n + 2 * t + e) * to_log2;
+              tops[i][x] = fmaxf(tops[i][x], v);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        float top = tops[i][x];
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         top = fmaxf(top, m[i][x]);
