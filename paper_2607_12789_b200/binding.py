@@ -547,12 +547,17 @@ class PagedCache:
 
     def attend(self, Q, table, lens, scale=None, flags=0, Y=None, lse=False, plan=None):
         """avq_cache_attend: the last queries Q [B*nq,H,d] of B sequences (``lens`` int32 [B] tokens in the pages ``table``
-        int32 [B, n]) over the cache.  Returns Y, or (Y, lse).  ``plan``: what ``plan`` made, else one is made here."""
+        int32 [B, n]) over the cache.  Returns Y, or (Y, lse).  ``plan``: what ``plan`` made, its scale and flags with it (given
+        here too, they have to be the same); else one is made here."""
         B = lens.shape[0]
         if plan is None:
             if B == 0 or Q.shape[0] % B:
                 raise ValueError("Q must hold the same number of rows for each of the sequences of lens")
             plan = self.plan(Q.shape[1], B, max(1, Q.shape[0] // B), scale, flags)
+        elif scale is not None and ctypes.c_float(scale).value != plan[0].scale:
+            raise ValueError(f"the plan's scale is {plan[0].scale}, not {scale}")
+        elif flags and flags != plan[0].flags:
+            raise ValueError(f"the plan's flags are {plan[0].flags}, not {flags}")
         heads, ws, pB, nq = plan
         if B != pB or len(table.shape) != 2:
             raise ValueError(f"lens must be [{pB}] and table [{pB}, n]")

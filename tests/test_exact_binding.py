@@ -1,0 +1,30 @@
+"""The binding of the exact operators: what it refuses before anything is launched (no GPU needed)."""
+import pytest
+import torch
+
+from paper_2607_12789_b200 import binding, build
+
+BF16 = torch.bfloat16
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    build.build()
+    return binding.lib()
+
+
+def _cached(B=2):
+    c = binding.PagedCache.empty(6, 16, 2, 64, device="cpu")
+    return c, torch.zeros(B, 4, 64, dtype=BF16), torch.zeros(B, 3, dtype=torch.int32), torch.full((B,), 5, dtype=torch.int32)
+
+
+def test_a_plan_with_another_scale_or_other_flags_is_refused():
+    c, Q, table, lens = _cached()
+    plan = c.plan(4, 2, scale=0.3, flags=binding.FLAG_SIMT)
+    for kw, what in ((dict(scale=0.125), "scale"), (dict(scale=0.0), "scale"), (dict(flags=16), "flags"),
+                     (dict(scale=0.3, flags=binding.FLAG_CAUSAL), "flags")):
+        with pytest.raises(ValueError, match=what):
+            c.attend(Q, table, lens, plan=plan, **kw)
+    for kw in ({}, dict(scale=0.3), dict(flags=binding.FLAG_SIMT), dict(scale=0.3, flags=binding.FLAG_SIMT)):
+        with pytest.raises(ValueError, match="CUDA device"):   # (these agree; the tensors are the CPU's)
+            c.attend(Q, table, lens, plan=plan, **kw)
