@@ -464,6 +464,8 @@ class PagedCache:
         for name, t in (("keys", keys), ("values", values)):
             if (tuple(t.shape), t.dtype) != want or not t.is_contiguous():
                 raise ValueError(f"{name} must be contiguous {want[1]} {want[0]}, not {t.dtype} {tuple(t.shape)}")
+        if keys.device != values.device:                   # (calls look at the keys' device alone)
+            raise ValueError(f"keys and values must be on one device, not on {keys.device} and {values.device}")
         self.keys, self.values, self.dtype = keys, values, dtype
         self.desc = AvqCache(keys.data_ptr(), values.data_ptr(), pages, page, Hk, d, code, bits)
         if int(lib().avq_cache_bytes(self.desc)) == 0:

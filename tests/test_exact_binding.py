@@ -28,3 +28,9 @@ def test_a_plan_with_another_scale_or_other_flags_is_refused():
     for kw in ({}, dict(scale=0.3), dict(flags=binding.FLAG_SIMT), dict(scale=0.3, flags=binding.FLAG_SIMT)):
         with pytest.raises(ValueError, match="CUDA device"):   # (these agree; the tensors are the CPU's)
             c.attend(Q, table, lens, plan=plan, **kw)
+
+
+def test_keys_and_values_on_different_devices_are_refused():
+    keys = torch.zeros(3, 2, 16, 64, dtype=BF16)
+    with pytest.raises(ValueError, match="device"):
+        binding.PagedCache(keys, keys.to("meta"), 16, 64)
