@@ -390,6 +390,14 @@ def _here(at, *ts):
             raise ValueError(f"tensors must be on the current CUDA device, not on {t.device}")
 
 
+def _check(header):
+    # (behind the work of the current device's stream: a header of another device would be read too early)
+    _here(torch._C._cuda_getDevice() if header.is_cuda else -2, header)
+    st = lib().avq_check(_ptr(header), _stream())
+    if st != 0:
+        raise AvqError(st, "avq_check")
+
+
 class ExactAttention:
     """avq_prompt_attend: softmax attention over packed sequences, planned for one set of heads.
 
@@ -442,9 +450,7 @@ class ExactAttention:
 
     def check(self) -> None:
         """avq_check: raises if a kernel left something out (unusable bounds) or gave up on a wait."""
-        st = lib().avq_check(_ptr(self.workspace), _stream())
-        if st != 0:
-            raise AvqError(st, "avq_check")
+        _check(self.workspace)
 
 
 class PagedCache:
@@ -584,6 +590,4 @@ class PagedCache:
     def check(self, plan=None) -> None:
         """avq_check of the cache's header, or of a plan's: raises if a kernel skipped a slot, position, length or page
         out of range."""
-        st = lib().avq_check(_ptr(self.header if plan is None else plan[1]), _stream())
-        if st != 0:
-            raise AvqError(st, "avq_check")
+        _check(self.header if plan is None else plan[1])

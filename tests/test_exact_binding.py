@@ -34,3 +34,17 @@ def test_keys_and_values_on_different_devices_are_refused():
     keys = torch.zeros(3, 2, 16, 64, dtype=BF16)
     with pytest.raises(ValueError, match="device"):
         binding.PagedCache(keys, keys.to("meta"), 16, 64)
+
+
+def test_a_check_away_from_the_workspace_s_device_is_refused(monkeypatch):
+    """The header is read behind the work of the current device's stream: work on another device would not be waited for."""
+    called = []
+    monkeypatch.setattr(binding, "_lib", type("L", (), {"avq_check": staticmethod(lambda *a: called.append(a) or 0)}))
+    monkeypatch.setattr(binding, "_raw_stream", lambda: 0)
+    att, c = object.__new__(binding.ExactAttention), object.__new__(binding.PagedCache)
+    att.workspace = c.header = torch.empty(256, dtype=torch.uint8)
+    for check in (att.check, c.check, lambda: c.check((None, att.workspace, 1, 1))):
+        with pytest.raises(ValueError, match="CUDA device"):
+            check()
+    assert not called
+
