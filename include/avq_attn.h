@@ -322,6 +322,14 @@ AVQ_API avq_status avq_prompt_attend(const avq_heads* heads, const void* Q, int6
                              int64_t k_stride, const void* V, int64_t v_stride, const int32_t* cu_q,
                              const int32_t* cu_k, int32_t S, int32_t Tq, int32_t Tk, void* Y, int64_t y_stride,
                              float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
+/* The same with the header and the room for partial results apart: scratch of avq_prompt_split_bytes() - 256 bytes, 256-byte
+ * aligned, or NULL and 0 (nothing is split then; calls of fewer than AVQ_PROMPT_SPLIT_KEYS keys never are).  Calls that may
+ * overlap may share a header; scratch is a call's own until its work is done. */
+#define AVQ_PROMPT_SPLIT_KEYS 2048
+AVQ_API avq_status avq_prompt_attend_scratch(const avq_heads* heads, const void* Q, int64_t q_stride, const void* K,
+                             int64_t k_stride, const void* V, int64_t v_stride, const int32_t* cu_q,
+                             const int32_t* cu_k, int32_t S, int32_t Tq, int32_t Tk, void* Y, int64_t y_stride,
+                             float* lse_out, void* header, void* scratch, size_t scratch_bytes, void* stream);
 
 /* A paged cache of keys and values.  Page p, head h starts at element (p * Hk + h) * page * d of `keys` and `values`
  * and holds `page` rows of d elements of `dtype` (bits: that type's width), or, with bits = 4, at byte
@@ -381,6 +389,12 @@ AVQ_API size_t avq_cache_attend_workspace_bytes(const avq_heads* heads, int32_t 
 AVQ_API avq_status avq_cache_attend(const avq_heads* heads, const avq_cache* cache, const void* Q, int64_t q_stride,
                             const int32_t* table, int32_t table_pages, const int32_t* lens, int32_t B, int32_t nq,
                             void* Y, int64_t y_stride, float* lse_out, void* workspace, size_t workspace_bytes,
+                            void* stream);
+/* The same with the header and the room for partial results apart: scratch of avq_cache_attend_workspace_bytes() - 256 bytes,
+ * 256-byte aligned.  Calls that may overlap may share a header; scratch is a call's own until its work is done. */
+AVQ_API avq_status avq_cache_attend_scratch(const avq_heads* heads, const avq_cache* cache, const void* Q, int64_t q_stride,
+                            const int32_t* table, int32_t table_pages, const int32_t* lens, int32_t B, int32_t nq,
+                            void* Y, int64_t y_stride, float* lse_out, void* header, void* scratch, size_t scratch_bytes,
                             void* stream);
 
 /* Waits for `stream`, reads the status word in the workspace header and clears it.

@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import threading
 
 import torch
 
@@ -17,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "lib", "libavq_attn.so")
 
 AVQ_F32, AVQ_BF16 = 0, 1
 FLAG_PARENT_STAYS, FLAG_SIMT, FLAG_CORRECTING, FLAG_CAUSAL = 1, 2, 4, 8
+PROMPT_SPLIT_KEYS = 2048       # AVQ_PROMPT_SPLIT_KEYS
 STATUS_NAMES = {0: "AVQ_OK", 1: "AVQ_ERR_NULL", 2: "AVQ_ERR_SHAPE", 3: "AVQ_ERR_UNSUPPORTED", 4: "AVQ_ERR_ALIGN",
                 5: "AVQ_ERR_WORKSPACE", 6: "AVQ_ERR_CUDA", 7: "AVQ_ERR_DEVICE_TIMEOUT", 8: "AVQ_ERR_INDEX"}
 
@@ -24,8 +26,9 @@ EXPORTS = ("avq_workspace_bytes", "avq_assign", "avq_aggregate", "avq_forward", 
            "avq_workspace_layout", "avq_check", "avq_status_string", "avq_version", "avq_forward_static",
            "avq_check_static", "avq_static_workspace_bytes", "avq_workspace_bytes_permuted",
            "avq_forward_permuted", "avq_codebook_update_workspace_bytes", "avq_codebook_update",
-           "avq_forward_tiled", "avq_prompt_workspace_bytes", "avq_prompt_split_bytes", "avq_prompt_attend", "avq_cache_bytes", "avq_cache_append",
-           "avq_cache_read", "avq_cache_attend_workspace_bytes", "avq_cache_attend")
+           "avq_forward_tiled", "avq_prompt_workspace_bytes", "avq_prompt_split_bytes", "avq_prompt_attend",
+           "avq_prompt_attend_scratch", "avq_cache_bytes", "avq_cache_append", "avq_cache_read",
+           "avq_cache_attend_workspace_bytes", "avq_cache_attend", "avq_cache_attend_scratch")
 
 
 class AvqProblem(ctypes.Structure):
@@ -100,6 +103,8 @@ def lib() -> ctypes.CDLL:
         L.avq_prompt_split_bytes.restype, L.avq_prompt_split_bytes.argtypes = sz, [ph]
         L.avq_prompt_attend.restype = i32
         L.avq_prompt_attend.argtypes = [ph, vp, i64, vp, i64, vp, i64, vp, vp, i32, i32, i32, vp, i64, vp, vp, sz, vp]
+        L.avq_prompt_attend_scratch.restype = i32
+        L.avq_prompt_attend_scratch.argtypes = [*L.avq_prompt_attend.argtypes[:-3], vp, vp, sz, vp]
         L.avq_cache_bytes.restype, L.avq_cache_bytes.argtypes = sz, [pc]
         L.avq_cache_append.restype = i32
         L.avq_cache_append.argtypes = [pc, vp, i64, vp, i64, vp, i32, ctypes.POINTER(AvqRotation), vp, i64, i32, vp,
@@ -109,6 +114,8 @@ def lib() -> ctypes.CDLL:
         L.avq_cache_attend_workspace_bytes.argtypes = [ph, i32, i32]
         L.avq_cache_attend.restype = i32
         L.avq_cache_attend.argtypes = [ph, pc, vp, i64, vp, i32, vp, i32, i32, vp, i64, vp, vp, sz, vp]
+        L.avq_cache_attend_scratch.restype = i32
+        L.avq_cache_attend_scratch.argtypes = [*L.avq_cache_attend.argtypes[:-3], vp, vp, sz, vp]
         L.avq_status_string.restype, L.avq_status_string.argtypes = ctypes.c_char_p, [i32]
         L.avq_version.restype, L.avq_version.argtypes = i32, []
         _lib = L
@@ -398,13 +405,39 @@ def _check(header):
         raise AvqError(st, "avq_check")
 
 
+class _Room:
+    """A plan's workspace: the header, which all of its calls share, and room for partial results.
+
+    The room is for calls on one stream, that of the first of them, and for one thread at a time (`lock`: a call is two
+    launches, and another's must not come between).  Calls on other streams and calls that are being captured take theirs
+    from the allocator: its blocks are that stream's or that graph's own.  So a plan may serve any number of them at once."""
+    __slots__ = ("workspace", "header", "rest", "bytes", "stream", "lock")
+
+    def __init__(self, n, device):
+        self.workspace = torch.empty(n, dtype=torch.uint8, device=device)
+        self.workspace[:256].zero_()
+        self.header = self.workspace.data_ptr()
+        self.rest, self.bytes, self.stream, self.lock = self.header + 256, n - 256, None, threading.Lock()
+
+    def scratch(self, stream):
+        """(Under `lock`) the address of the room that a call on this stream, the current one, takes; whom to keep till then."""
+        if not torch._C._cuda_isCurrentStreamCapturing():
+            if self.stream is None:
+                self.stream = stream
+                self.workspace.record_stream(torch.cuda.current_stream())
+            if self.stream == stream:
+                return self.rest, None
+        room = self.workspace.new_empty(self.bytes)
+        return room.data_ptr(), room
+
+
 class ExactAttention:
     """avq_prompt_attend: softmax attention over packed sequences, planned for one set of heads.
 
     ``ExactAttention(H, Hk, d)(Q, K, V, cu_q, cu_k=None)`` takes Q [Tq,H,d], K, V [Tk,Hk,d] (rows may be views of a
     wider tensor) and the int32 bounds [S+1] of the sequences' queries and keys, and returns Y [Tq,H,d], with ``lse`` also
     the log of every query's sum, float32 [Tq,H].  ``split``: keep room (20 or 40 MB) for the parts of calls of few queries
-    over many keys; calls that may overlap then need plans of their own.  Rows outside all sequences are left as they are (in a Y made here: anything)."""
+    over many keys; calls on a second stream and captured ones take as much again for themselves.  Rows outside all sequences are left as they are (in a Y made here: anything)."""
 
     def __init__(self, H, Hk, d, dtype=torch.bfloat16, scale=None, causal=True, flags=0, device="cuda", split=True):
         code = {torch.float32: AVQ_F32, torch.bfloat16: AVQ_BF16}.get(dtype)
@@ -417,8 +450,8 @@ class ExactAttention:
         if n == 0:
             raise AvqError(lib().avq_prompt_attend(self.heads, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0) or 3,
                            "avq_prompt_workspace_bytes")
-        self.workspace, self.bytes, self.sizes = torch.empty(n, dtype=torch.uint8, device=device), n, (H, Hk, d)
-        self.workspace[:256].zero_()
+        self.room, self.sizes = _Room(n, device), (H, Hk, d)
+        self.workspace = self.room.workspace
 
     def __call__(self, Q, K, V, cu_q, cu_k=None, Y=None, lse=False):
         h, dtype = self.heads, self.dtype
@@ -437,20 +470,30 @@ class ExactAttention:
         else:
             ys = _rows("Y", Y, H, d, dtype, Tq)
         L = Q.new_empty((Tq, H), dtype=torch.float32) if lse else None
-        st = self._call(h, Q.data_ptr(), qs, K.data_ptr(), ks, V.data_ptr(), vs, cu_q.data_ptr(),
-                        None if cu_k is None else cu_k.data_ptr(), S, Tq, Tk, Y.data_ptr(), ys, L.data_ptr() if lse else None,
-                        self.workspace.data_ptr(), self.bytes, torch._C._cuda_getCurrentRawStream(at))
+        stream, room = torch._C._cuda_getCurrentRawStream(at), self.room
+        args = (h, Q.data_ptr(), qs, K.data_ptr(), ks, V.data_ptr(), vs, cu_q.data_ptr(),
+                None if cu_k is None else cu_k.data_ptr(), S, Tq, Tk, Y.data_ptr(), ys, L.data_ptr() if lse else None, room.header)
+        if Tk < PROMPT_SPLIT_KEYS or not room.bytes:        # nothing is split: no partial results
+            st = self._call(*args, None, 0, stream)
+        else:
+            with room.lock:
+                rest, kept = room.scratch(stream)
+                st = self._call(*args, rest, room.bytes, stream)
         if st != 0:
             raise AvqError(st, "avq_prompt_attend")
         return (Y, L) if lse else Y
 
     @property
     def _call(self):
-        return (_lib or lib()).avq_prompt_attend
+        return (_lib or lib()).avq_prompt_attend_scratch
 
     def check(self) -> None:
         """avq_check: raises if a kernel left something out (unusable bounds) or gave up on a wait."""
         _check(self.workspace)
+
+
+class CachePlan(tuple):
+    """What ``PagedCache.plan`` makes: (heads, workspace, B, nq), and `room`, the workspace's use."""
 
 
 class PagedCache:
@@ -542,16 +585,18 @@ class PagedCache:
         return K, V
 
     def plan(self, H, B, nq=1, scale=None, flags=0):
-        """Workspace and heads of repeated ``attend`` calls of B sequences with nq queries each."""
+        """Workspace and heads of repeated ``attend`` calls of B sequences with nq queries each.  Calls on a second stream and
+        captured ones take as much room again for themselves."""
         c = self.desc
         heads = AvqHeads(H, c.Hk, c.d, c.dtype, float(scale) if scale is not None else 1.0 / math.sqrt(c.d), flags)
         n = int(lib().avq_cache_attend_workspace_bytes(heads, B, nq))
         if n == 0:
             raise AvqError(lib().avq_cache_attend(heads, c, 0, 0, 0, 0, 0, B, nq, 0, 0, 0, 0, 0, 0) or 3,
                            "avq_cache_attend_workspace_bytes")
-        ws = torch.empty(n, dtype=torch.uint8, device=self.keys.device)
-        ws[:256].zero_()
-        return heads, ws, B, nq
+        room = _Room(n, self.keys.device)
+        plan = CachePlan((heads, room.workspace, B, nq))
+        plan.room = room
+        return plan
 
     def attend(self, Q, table, lens, scale=None, flags=0, Y=None, lse=False, plan=None):
         """avq_cache_attend: the last queries Q [B*nq,H,d] of B sequences (``lens`` int32 [B] tokens in the pages ``table``
@@ -567,6 +612,7 @@ class PagedCache:
         elif flags and flags != plan[0].flags:
             raise ValueError(f"the plan's flags are {plan[0].flags}, not {flags}")
         heads, ws, pB, nq = plan
+        room = plan.room
         if B != pB or len(table.shape) != 2:
             raise ValueError(f"lens must be [{pB}] and table [{pB}, n]")
         H, d, dtype, T, pages = heads.H, self.sizes[1], self.dtype, B * nq, table.shape[1]
@@ -580,9 +626,12 @@ class PagedCache:
         else:
             ys = _rows("Y", Y, H, d, dtype, T)
         L = Q.new_empty((T, H), dtype=torch.float32) if lse else None
-        st = (_lib or lib()).avq_cache_attend(heads, self.desc, Q.data_ptr(), qs, table.data_ptr(), pages, lens.data_ptr(), B, nq,
-                                              Y.data_ptr(), ys, L.data_ptr() if lse else None, ws.data_ptr(), ws.numel(),
-                                              torch._C._cuda_getCurrentRawStream(at))
+        stream = torch._C._cuda_getCurrentRawStream(at)
+        with room.lock:
+            scratch, kept = room.scratch(stream)
+            st = (_lib or lib()).avq_cache_attend_scratch(heads, self.desc, Q.data_ptr(), qs, table.data_ptr(), pages, lens.data_ptr(), B,
+                                                          nq, Y.data_ptr(), ys, L.data_ptr() if lse else None, room.header, scratch,
+                                                          room.bytes, stream)
         if st != 0:
             raise AvqError(st, "avq_cache_attend")
         return (Y, L) if lse else Y

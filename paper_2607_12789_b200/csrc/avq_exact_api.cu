@@ -71,6 +71,67 @@ size_t records_bytes(const avq_heads& h, int32_t B, int32_t nq) {   // a record 
     if (s_ != AVQ_OK) return s_;        \
   } while (0)
 
+// The checks and dispatch of avq_prompt_attend and avq_prompt_attend_scratch; header and room are checked behind the rows.
+avq_status prompt(const avq_heads* heads, const void* Q, int64_t q_stride, const void* K, int64_t k_stride, const void* V,
+                  int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k, int32_t S, int32_t Tq, int32_t Tk, void* Y,
+                  int64_t y_stride, float* lse_out, void* header, void* parts, size_t parts_bytes, void* stream) {
+  AVQ_TRY(validate_prompt(heads));
+  if (S < 0 || Tq < 0 || Tk < 0 || (!cu_k && Tk != Tq)) return AVQ_ERR_SHAPE;
+  if (S == 0 || Tq == 0) return AVQ_OK;
+  if (!cu_q) return AVQ_ERR_NULL;
+  const avq_heads& h = *heads;
+  AVQ_TRY(validate_rows(Q, q_stride, h.H, h.d, h.dtype));
+  AVQ_TRY(validate_rows(Y, y_stride, h.H, h.d, h.dtype));
+  if (Tk > 0) {
+    AVQ_TRY(validate_rows(K, k_stride, h.Hk, h.d, h.dtype));
+    AVQ_TRY(validate_rows(V, v_stride, h.Hk, h.d, h.dtype));
+  }
+  if (!header) return AVQ_ERR_WORKSPACE;
+  AVQ_TRY(validate_header(header));
+  AVQ_TRY(validate_header(parts));
+  if (too_many(Tq) || too_many(Tk)) return AVQ_ERR_UNSUPPORTED;
+  if (S > (1 << 16)) return AVQ_ERR_UNSUPPORTED;         // (every CTA passes over the sequences behind its own)
+  const size_t room = avq_prompt_split_bytes(heads) - 256;
+  const PromptArgs a = {Q, K, V, Y, lse_out, cu_q, cu_k, q_stride, k_stride, v_stride, y_stride, h.H, h.Hk, h.d, S, Tq, Tk,
+                        (h.flags & AVQ_FLAG_CAUSAL) ? 1 : 0, h.scale, static_cast<int32_t*>(header),
+                        room > 0 && parts_bytes >= room ? static_cast<float*>(parts) : nullptr};
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (!tensor_path(h) || (h.dtype == AVQ_F32 && h.d != 64 && h.d != 128)) return simt_prompt(a, h.dtype, st);
+  return h.dtype == AVQ_F32 ? tc_prompt_f32(a, st) : tc_prompt(a, st);
+}
+
+// The same of avq_cache_attend and avq_cache_attend_scratch.
+avq_status cached(const avq_heads* heads, const avq_cache* cache, const void* Q, int64_t q_stride, const int32_t* table,
+                  int32_t table_pages, const int32_t* lens, int32_t B, int32_t nq, void* Y, int64_t y_stride, float* lse_out,
+                  void* header, void* scratch, size_t scratch_bytes, void* stream) {
+  AVQ_TRY(validate_cached(heads, B, nq));
+  AVQ_TRY(validate_cache(cache));
+  const avq_heads& h = *heads;
+  const avq_cache& c = *cache;
+  if (c.Hk != h.Hk || c.d != h.d || c.dtype != h.dtype || table_pages < 0) return AVQ_ERR_SHAPE;
+  if (too_many((int64_t)table_pages * c.page)) return AVQ_ERR_UNSUPPORTED;
+  if (B == 0) return AVQ_OK;
+  if (!c.keys || !c.values || !lens || (table_pages > 0 && !table)) return AVQ_ERR_NULL;
+  if (!aligned16(c.keys) || !aligned16(c.values)) return AVQ_ERR_ALIGN;
+  AVQ_TRY(validate_rows(Q, q_stride, h.H, h.d, h.dtype));
+  AVQ_TRY(validate_rows(Y, y_stride, h.H, h.d, h.dtype));
+  if (!header || !scratch || scratch_bytes < avq_cache_attend_workspace_bytes(heads, B, nq) - 256) return AVQ_ERR_WORKSPACE;
+  AVQ_TRY(validate_header(header));
+  AVQ_TRY(validate_header(scratch));
+  const CachedArgs a = {Q, c.keys, c.values, Y, lse_out, reinterpret_cast<float*>(static_cast<char*>(scratch) + records_bytes(h, B, nq)),
+                        static_cast<int2*>(scratch),
+                        table, lens, q_stride, y_stride, h.H, h.Hk, h.d, B, nq, c.pages, c.page, table_pages, h.scale,
+                        static_cast<int32_t*>(header)};
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return tensor_path(h) ? tc_cached(a, h.dtype, c.bits, st) : simt_cached(a, h.dtype, c.bits, st);
+}
+
+// What follows the header of a workspace of `bytes` bytes, its size in `rest` (0 and null if it does not even hold a header).
+void* behind_header(void* workspace, size_t bytes, size_t* rest) {
+  *rest = workspace && bytes >= 256 ? bytes - 256 : 0;
+  return *rest ? static_cast<char*>(workspace) + 256 : nullptr;
+}
+
 }  // namespace
 }  // namespace exact
 }  // namespace avq
@@ -91,28 +152,18 @@ avq_status avq_prompt_attend(const avq_heads* heads, const void* Q, int64_t q_st
                              const void* V, int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k, int32_t S,
                              int32_t Tq, int32_t Tk, void* Y, int64_t y_stride, float* lse_out, void* workspace,
                              size_t workspace_bytes, void* stream) {
-  AVQ_TRY(validate_prompt(heads));
-  if (S < 0 || Tq < 0 || Tk < 0 || (!cu_k && Tk != Tq)) return AVQ_ERR_SHAPE;
-  if (S == 0 || Tq == 0) return AVQ_OK;
-  if (!cu_q) return AVQ_ERR_NULL;
-  const avq_heads& h = *heads;
-  AVQ_TRY(validate_rows(Q, q_stride, h.H, h.d, h.dtype));
-  AVQ_TRY(validate_rows(Y, y_stride, h.H, h.d, h.dtype));
-  if (Tk > 0) {
-    AVQ_TRY(validate_rows(K, k_stride, h.Hk, h.d, h.dtype));
-    AVQ_TRY(validate_rows(V, v_stride, h.Hk, h.d, h.dtype));
-  }
-  if (!workspace || workspace_bytes < 256) return AVQ_ERR_WORKSPACE;
-  AVQ_TRY(validate_header(workspace));
-  if (too_many(Tq) || too_many(Tk)) return AVQ_ERR_UNSUPPORTED;
-  if (S > (1 << 16)) return AVQ_ERR_UNSUPPORTED;         // (every CTA passes over the sequences behind its own)
-  const PromptArgs a = {Q, K, V, Y, lse_out, cu_q, cu_k, q_stride, k_stride, v_stride, y_stride, h.H, h.Hk, h.d, S, Tq, Tk,
-                        (h.flags & AVQ_FLAG_CAUSAL) ? 1 : 0, h.scale, static_cast<int32_t*>(workspace),
-                        workspace_bytes > 256 && workspace_bytes >= avq_prompt_split_bytes(heads)
-                            ? reinterpret_cast<float*>(static_cast<char*>(workspace) + 256) : nullptr};
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (!tensor_path(h) || (h.dtype == AVQ_F32 && h.d != 64 && h.d != 128)) return simt_prompt(a, h.dtype, st);
-  return h.dtype == AVQ_F32 ? tc_prompt_f32(a, st) : tc_prompt(a, st);
+  size_t rest;
+  void* parts = behind_header(workspace, workspace_bytes, &rest);
+  return prompt(heads, Q, q_stride, K, k_stride, V, v_stride, cu_q, cu_k, S, Tq, Tk, Y, y_stride, lse_out,
+                workspace_bytes >= 256 ? workspace : nullptr, parts, rest, stream);
+}
+
+avq_status avq_prompt_attend_scratch(const avq_heads* heads, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                             const void* V, int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k, int32_t S,
+                             int32_t Tq, int32_t Tk, void* Y, int64_t y_stride, float* lse_out, void* header, void* scratch,
+                             size_t scratch_bytes, void* stream) {
+  return prompt(heads, Q, q_stride, K, k_stride, V, v_stride, cu_q, cu_k, S, Tq, Tk, Y, y_stride, lse_out, header, scratch,
+                scratch_bytes, stream);
 }
 
 size_t avq_cache_bytes(const avq_cache* cache) {
@@ -178,25 +229,15 @@ size_t avq_cache_attend_workspace_bytes(const avq_heads* heads, int32_t B, int32
 avq_status avq_cache_attend(const avq_heads* heads, const avq_cache* cache, const void* Q, int64_t q_stride,
                             const int32_t* table, int32_t table_pages, const int32_t* lens, int32_t B, int32_t nq, void* Y,
                             int64_t y_stride, float* lse_out, void* workspace, size_t workspace_bytes, void* stream) {
-  AVQ_TRY(validate_cached(heads, B, nq));
-  AVQ_TRY(validate_cache(cache));
-  const avq_heads& h = *heads;
-  const avq_cache& c = *cache;
-  if (c.Hk != h.Hk || c.d != h.d || c.dtype != h.dtype || table_pages < 0) return AVQ_ERR_SHAPE;
-  if (too_many((int64_t)table_pages * c.page)) return AVQ_ERR_UNSUPPORTED;
-  if (B == 0) return AVQ_OK;
-  if (!c.keys || !c.values || !lens || (table_pages > 0 && !table)) return AVQ_ERR_NULL;
-  if (!aligned16(c.keys) || !aligned16(c.values)) return AVQ_ERR_ALIGN;
-  AVQ_TRY(validate_rows(Q, q_stride, h.H, h.d, h.dtype));
-  AVQ_TRY(validate_rows(Y, y_stride, h.H, h.d, h.dtype));
-  if (!workspace || workspace_bytes < avq_cache_attend_workspace_bytes(heads, B, nq)) return AVQ_ERR_WORKSPACE;
-  AVQ_TRY(validate_header(workspace));
-  const CachedArgs a = {Q, c.keys, c.values, Y, lse_out, reinterpret_cast<float*>(static_cast<char*>(workspace) + 256 + records_bytes(h, B, nq)),
-                        reinterpret_cast<int2*>(static_cast<char*>(workspace) + 256),
-                        table, lens, q_stride, y_stride, h.H, h.Hk, h.d, B, nq, c.pages, c.page, table_pages, h.scale,
-                        static_cast<int32_t*>(workspace)};
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return tensor_path(h) ? tc_cached(a, h.dtype, c.bits, st) : simt_cached(a, h.dtype, c.bits, st);
+  size_t rest;
+  void* scratch = behind_header(workspace, workspace_bytes, &rest);
+  return cached(heads, cache, Q, q_stride, table, table_pages, lens, B, nq, Y, y_stride, lse_out, workspace, scratch, rest, stream);
+}
+
+avq_status avq_cache_attend_scratch(const avq_heads* heads, const avq_cache* cache, const void* Q, int64_t q_stride,
+                            const int32_t* table, int32_t table_pages, const int32_t* lens, int32_t B, int32_t nq, void* Y,
+                            int64_t y_stride, float* lse_out, void* header, void* scratch, size_t scratch_bytes, void* stream) {
+  return cached(heads, cache, Q, q_stride, table, table_pages, lens, B, nq, Y, y_stride, lse_out, header, scratch, scratch_bytes, stream);
 }
 
 }  // extern "C"

@@ -35,7 +35,7 @@ constexpr int kTile = 128, kThreads = 384, kLoader = 8, kIssuer = 9, kGuards = 6
 constexpr int kMost = 96;                                  // weights of a tile that the product starts with
 constexpr int kReady = 8;                                  // value tiles that the guards can be ahead by, at least
 constexpr float kRaise = 8.f;
-constexpr int kSplitBelow = 148, kSplitKeys = 2048, kLeastTiles = 4, kSetupTiles = 2;   // when pieces are split, and into parts of what size at least
+constexpr int kSplitBelow = 148, kSplitKeys = AVQ_PROMPT_SPLIT_KEYS, kLeastTiles = 4, kSetupTiles = 2;   // when pieces are split, and into parts of what size at least
 constexpr int kFewRegs = 80, kManyRegs = 208;              // per thread of warps 8-11, of warps 0-7
 template <int D> __host__ __device__ constexpr int ring_slots() { return D == 128 ? 5 : 10; }
 template <int D> __host__ __device__ constexpr int tile_bytes() { return kTile * D * 2; }

@@ -48,3 +48,48 @@ def test_a_check_away_from_the_workspace_s_device_is_refused(monkeypatch):
             check()
     assert not called
 
+
+
+def test_a_plan_s_room_is_one_stream_s_alone(monkeypatch):
+    """The first eager call's stream has the plan's own room; other streams and captures get room of the allocator's each time."""
+    capturing = [True]
+    monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: capturing[0], raising=False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: None)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, s: None)
+    for room, size in ((binding.ExactAttention(4, 2, 64, device="cpu").room, 4 * 2 * 148 * 256 * 66),
+                       (_cached()[0].plan(4, 2).room, binding.lib().avq_cache_attend_workspace_bytes(_cached()[0].plan(4, 2)[0], 2, 1) - 256)):
+        own = room.workspace.data_ptr() + 256
+        capturing[0] = True
+        at, kept = room.scratch(7)                          # a capture does not make its stream the plan's
+        assert at == kept.data_ptr() != own and kept.numel() == room.bytes == size
+        capturing[0] = False
+        assert room.scratch(5) == (own, None) and room.scratch(5) == (own, None)
+        a, b = room.scratch(6), room.scratch(7)
+        assert len({own, a[0], b[0]}) == 3 and a[1].numel() == b[1].numel() == size
+        capturing[0] = True
+        assert room.scratch(5)[0] != own
+    assert binding.ExactAttention(4, 2, 64, device="cpu", split=False).room.bytes == 0
+
+
+def test_the_header_s_constant_and_the_binding_s_agree():
+    import os
+    import re
+    hdr = open(os.path.join(os.path.dirname(binding.__file__), "..", "include", "avq_attn.h")).read()
+    assert int(re.search(r"#define AVQ_PROMPT_SPLIT_KEYS (\d+)", hdr).group(1)) == binding.PROMPT_SPLIT_KEYS
+
+
+def test_header_and_scratch_apart_are_refused_where_unusable(lib):
+    OK, h = 0x1000, binding.AvqHeads(4, 2, 64, binding.AVQ_BF16, 0.125, 0)
+    prompt = lambda header=OK, scratch=OK, n=1 << 30: lib.avq_prompt_attend_scratch(
+        h, OK, 256, OK, 128, OK, 128, OK, OK, 1, 5, 9, 0, 256, 0, header, scratch, n, 0)
+    assert prompt() == 1                                    # (no Y: rows are looked at first)
+    prompt = lambda header=OK, scratch=OK, n=1 << 30: lib.avq_prompt_attend_scratch(
+        h, OK, 256, OK, 128, OK, 128, OK, OK, 1, 5, 1 << 30, OK, 256, 0, header, scratch, n, 0)
+    assert prompt(header=0) == 5 and prompt(header=0x1080) == 4 and prompt(scratch=0x1010) == 4
+    assert prompt() == 3 and prompt(scratch=0, n=0) == 3    # (so many keys are refused: nothing is launched)
+    c = binding.AvqCache(OK, OK, 10, 16, 2, 64, binding.AVQ_BF16, 16)
+    n = lib.avq_cache_attend_workspace_bytes(h, 3, 1) - 256
+    call = lambda header=OK, scratch=OK, n=n, Y=OK: lib.avq_cache_attend_scratch(
+        h, c, OK, 256, OK, 4, OK, 3, 1, Y, 256, 0, header, scratch, n, 0)
+    assert call(header=0) == 5 and call(scratch=0) == 5 and call(n=n - 1) == 5 and call(header=0x1010) == 4
+    assert call(scratch=0x1010) == 4 and call(Y=0) == 1
