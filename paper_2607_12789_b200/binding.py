@@ -584,15 +584,20 @@ class PagedCache:
             raise AvqError(st, "avq_cache_read")
         return K, V
 
-    def plan(self, H, B, nq=1, scale=None, flags=0):
-        """Workspace and heads of repeated ``attend`` calls of B sequences with nq queries each.  Calls on a second stream and
-        captured ones take as much room again for themselves."""
+    def _heads(self, H, B, nq, scale, flags):
+        """The heads of such calls, and the bytes of their workspace."""
         c = self.desc
         heads = AvqHeads(H, c.Hk, c.d, c.dtype, float(scale) if scale is not None else 1.0 / math.sqrt(c.d), flags)
         n = int(lib().avq_cache_attend_workspace_bytes(heads, B, nq))
         if n == 0:
             raise AvqError(lib().avq_cache_attend(heads, c, 0, 0, 0, 0, 0, B, nq, 0, 0, 0, 0, 0, 0) or 3,
                            "avq_cache_attend_workspace_bytes")
+        return heads, n
+
+    def plan(self, H, B, nq=1, scale=None, flags=0):
+        """Workspace and heads of repeated ``attend`` calls of B sequences with nq queries each.  Calls on a second stream and
+        captured ones take as much room again for themselves."""
+        heads, n = self._heads(H, B, nq, scale, flags)
         room = _Room(n, self.keys.device)
         plan = CachePlan((heads, room.workspace, B, nq))
         plan.room = room
@@ -601,18 +606,20 @@ class PagedCache:
     def attend(self, Q, table, lens, scale=None, flags=0, Y=None, lse=False, plan=None):
         """avq_cache_attend: the last queries Q [B*nq,H,d] of B sequences (``lens`` int32 [B] tokens in the pages ``table``
         int32 [B, n]) over the cache.  Returns Y, or (Y, lse).  ``plan``: what ``plan`` made, its scale and flags with it (given
-        here too, they have to be the same); else one is made here."""
+        here too, they have to be the same).  Without one, `check` without one tells what the call left out."""
         B = lens.shape[0]
         if plan is None:
             if B == 0 or Q.shape[0] % B:
                 raise ValueError("Q must hold the same number of rows for each of the sequences of lens")
-            plan = self.plan(Q.shape[1], B, max(1, Q.shape[0] // B), scale, flags)
+            pB, nq, room, header = B, max(1, Q.shape[0] // B), None, self.header
+            heads, n = self._heads(Q.shape[1], B, nq, scale, flags)
         elif scale is not None and ctypes.c_float(scale).value != plan[0].scale:
             raise ValueError(f"the plan's scale is {plan[0].scale}, not {scale}")
         elif flags and flags != plan[0].flags:
             raise ValueError(f"the plan's flags are {plan[0].flags}, not {flags}")
-        heads, ws, pB, nq = plan
-        room = plan.room
+        else:
+            heads, header, pB, nq = plan
+            room = plan.room
         if B != pB or len(table.shape) != 2:
             raise ValueError(f"lens must be [{pB}] and table [{pB}, n]")
         H, d, dtype, T, pages = heads.H, self.sizes[1], self.dtype, B * nq, table.shape[1]
@@ -620,23 +627,28 @@ class PagedCache:
         _ints("lens", lens, (B,))
         _ints("table", table, (B, pages))
         at = torch._C._cuda_getDevice() if Q.is_cuda else -2
-        _here(at, Q, table, lens, Y, self.keys, ws)
+        _here(at, Q, table, lens, Y, self.keys, header)
         if Y is None:
             Y, ys = Q.new_empty((T, H, d)), H * d
         else:
             ys = _rows("Y", Y, H, d, dtype, T)
         L = Q.new_empty((T, H), dtype=torch.float32) if lse else None
         stream = torch._C._cuda_getCurrentRawStream(at)
-        with room.lock:
-            scratch, kept = room.scratch(stream)
-            st = (_lib or lib()).avq_cache_attend_scratch(heads, self.desc, Q.data_ptr(), qs, table.data_ptr(), pages, lens.data_ptr(), B,
-                                                          nq, Y.data_ptr(), ys, L.data_ptr() if lse else None, room.header, scratch,
-                                                          room.bytes, stream)
+        call = (_lib or lib()).avq_cache_attend_scratch
+        args = (heads, self.desc, Q.data_ptr(), qs, table.data_ptr(), pages, lens.data_ptr(), B, nq, Y.data_ptr(), ys,
+                L.data_ptr() if lse else None, header.data_ptr())
+        if room is None:
+            scratch = header.new_empty(n - 256)
+            st = call(*args, scratch.data_ptr(), n - 256, stream)
+        else:
+            with room.lock:
+                scratch, kept = room.scratch(stream)
+                st = call(*args, scratch, room.bytes, stream)
         if st != 0:
             raise AvqError(st, "avq_cache_attend")
         return (Y, L) if lse else Y
 
     def check(self, plan=None) -> None:
-        """avq_check of the cache's header, or of a plan's: raises if a kernel skipped a slot, position, length or page
-        out of range."""
+        """avq_check of the cache's header (append, read, attend without a plan), or of a plan's: raises if a kernel skipped a
+        slot, position, length or page out of range."""
         _check(self.header if plan is None else plan[1])

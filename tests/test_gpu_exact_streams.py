@@ -112,3 +112,21 @@ def test_one_plan_by_two_threads(case, same):
         t.join()
     assert not errors
     _check(want, out)
+
+
+@pytest.mark.parametrize("flags", [0, binding.FLAG_SIMT], ids=["tc", "simt"])
+def test_bad_pages_and_lengths_of_calls_without_a_plan_are_reported(flags):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(227)
+    c = binding.PagedCache.empty(4, 16, 2, 64)
+    q = torch.randn(2, 4, 64, device="cuda", generator=g).to(BF16)
+    table = _ints([[0, 1], [2, 3]])
+    good = c.attend(q, table, _ints([20, 32]), flags=flags)
+    c.check()
+    assert torch.equal(good, c.attend(q, table, _ints([20, 32]), flags=flags, plan=c.plan(4, 2, flags=flags)))
+    for t, n in ((_ints([[0, 4], [2, 3]]), [20, 32]), (_ints([[0, 1], [2, -1]]), [20, 32]), (table, [33, 32]), (table, [20, -1])):
+        c.attend(q, t, _ints(n), flags=flags)
+        c.attend(q, table, _ints([20, 32]), flags=flags)    # (a good call behind it takes nothing back)
+        with pytest.raises(binding.AvqError, match="AVQ_ERR_INDEX"):
+            c.check()
+        c.check()                                           # reported once
