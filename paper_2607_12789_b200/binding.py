@@ -6,6 +6,7 @@ has not been built the first call raises - there is no CPU or torch fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -405,6 +406,13 @@ def _check(header):
         raise AvqError(st, "avq_check")
 
 
+def _capturing():
+    return torch._C._cuda_isCurrentStreamCapturing()
+
+
+_NO_LOCK = contextlib.nullcontext()                        # (a call with room of its own waits for nobody)
+
+
 class _Room:
     """A plan's workspace: the header, which all of its calls share, and room for partial results.
 
@@ -421,14 +429,18 @@ class _Room:
 
     def scratch(self, stream):
         """(Under `lock`) the address of the room that a call on this stream, the current one, takes; whom to keep till then."""
-        if not torch._C._cuda_isCurrentStreamCapturing():
+        if not _capturing():
+            if self.stream == stream:
+                return self.rest, None
             if self.stream is None:
                 self.stream = stream
                 self.workspace.record_stream(torch.cuda.current_stream())
-            if self.stream == stream:
                 return self.rest, None
         room = self.workspace.new_empty(self.bytes)
         return room.data_ptr(), room
+
+    def __reduce__(self):                                  # (a copy has room and a header of its own)
+        return _Room, (256 + self.bytes, self.workspace.device)
 
 
 class ExactAttention:
@@ -437,7 +449,8 @@ class ExactAttention:
     ``ExactAttention(H, Hk, d)(Q, K, V, cu_q, cu_k=None)`` takes Q [Tq,H,d], K, V [Tk,Hk,d] (rows may be views of a
     wider tensor) and the int32 bounds [S+1] of the sequences' queries and keys, and returns Y [Tq,H,d], with ``lse`` also
     the log of every query's sum, float32 [Tq,H].  ``split``: keep room (20 or 40 MB) for the parts of calls of few queries
-    over many keys; calls on a second stream and captured ones take as much again for themselves.  Rows outside all sequences are left as they are (in a Y made here: anything)."""
+    over many keys; calls on a second stream and captured ones take as much again for themselves.
+    Rows outside all sequences are left as they are (in a Y made here: anything).  A plan has to outlive its captured graphs."""
 
     def __init__(self, H, Hk, d, dtype=torch.bfloat16, scale=None, causal=True, flags=0, device="cuda", split=True):
         code = {torch.float32: AVQ_F32, torch.bfloat16: AVQ_BF16}.get(dtype)
@@ -471,21 +484,22 @@ class ExactAttention:
             ys = _rows("Y", Y, H, d, dtype, Tq)
         L = Q.new_empty((Tq, H), dtype=torch.float32) if lse else None
         stream, room = torch._C._cuda_getCurrentRawStream(at), self.room
-        args = (h, Q.data_ptr(), qs, K.data_ptr(), ks, V.data_ptr(), vs, cu_q.data_ptr(),
-                None if cu_k is None else cu_k.data_ptr(), S, Tq, Tk, Y.data_ptr(), ys, L.data_ptr() if lse else None, room.header)
-        if Tk < PROMPT_SPLIT_KEYS or not room.bytes:        # nothing is split: no partial results
-            st = self._call(*args, None, 0, stream)
-        else:
-            with room.lock:
-                rest, kept = room.scratch(stream)
-                st = self._call(*args, rest, room.bytes, stream)
+        with room.lock:
+            if Tk < PROMPT_SPLIT_KEYS or not room.bytes:    # nothing is split: no partial results
+                scratch, n = None, 0
+            else:
+                (scratch, kept), n = room.scratch(stream), room.bytes
+            st = (_lib or lib()).avq_prompt_attend_scratch(
+                h, Q.data_ptr(), qs, K.data_ptr(), ks, V.data_ptr(), vs, cu_q.data_ptr(), None if cu_k is None else cu_k.data_ptr(),
+                S, Tq, Tk, Y.data_ptr(), ys, L.data_ptr() if lse else None, room.header, scratch, n, stream)
         if st != 0:
             raise AvqError(st, "avq_prompt_attend")
         return (Y, L) if lse else Y
 
-    @property
-    def _call(self):
-        return (_lib or lib()).avq_prompt_attend_scratch
+    def __reduce__(self):
+        h = self.heads
+        return type(self), (h.H, h.Hk, h.d, self.dtype, h.scale, bool(h.flags & FLAG_CAUSAL), h.flags & ~FLAG_CAUSAL, self.workspace.device,
+                            self.room.bytes > 0)
 
     def check(self) -> None:
         """avq_check: raises if a kernel left something out (unusable bounds) or gave up on a wait."""
@@ -493,7 +507,15 @@ class ExactAttention:
 
 
 class CachePlan(tuple):
-    """What ``PagedCache.plan`` makes: (heads, workspace, B, nq), and `room`, the workspace's use."""
+    """What ``PagedCache.plan`` makes: (heads, workspace, B, nq), and `room`, whose the workspace is."""
+
+    def __new__(cls, heads, room, B, nq):
+        plan = super().__new__(cls, (heads, room.workspace, B, nq))
+        plan.room = room
+        return plan
+
+    def __reduce__(self):
+        return CachePlan, (self[0], self.room, self[2], self[3])
 
 
 class PagedCache:
@@ -596,12 +618,9 @@ class PagedCache:
 
     def plan(self, H, B, nq=1, scale=None, flags=0):
         """Workspace and heads of repeated ``attend`` calls of B sequences with nq queries each.  Calls on a second stream and
-        captured ones take as much room again for themselves."""
+        captured ones take as much room again for themselves.  A plan has to outlive its captured graphs."""
         heads, n = self._heads(H, B, nq, scale, flags)
-        room = _Room(n, self.keys.device)
-        plan = CachePlan((heads, room.workspace, B, nq))
-        plan.room = room
-        return plan
+        return CachePlan(heads, _Room(n, self.keys.device), B, nq)
 
     def attend(self, Q, table, lens, scale=None, flags=0, Y=None, lse=False, plan=None):
         """avq_cache_attend: the last queries Q [B*nq,H,d] of B sequences (``lens`` int32 [B] tokens in the pages ``table``
@@ -611,8 +630,9 @@ class PagedCache:
         if plan is None:
             if B == 0 or Q.shape[0] % B:
                 raise ValueError("Q must hold the same number of rows for each of the sequences of lens")
-            pB, nq, room, header = B, max(1, Q.shape[0] // B), None, self.header
+            pB, nq, room, header, lock = B, max(1, Q.shape[0] // B), None, self.header, _NO_LOCK
             heads, n = self._heads(Q.shape[1], B, nq, scale, flags)
+            n, header_at = n - 256, header.data_ptr()
         elif scale is not None and ctypes.c_float(scale).value != plan[0].scale:
             raise ValueError(f"the plan's scale is {plan[0].scale}, not {scale}")
         elif flags and flags != plan[0].flags:
@@ -620,6 +640,7 @@ class PagedCache:
         else:
             heads, header, pB, nq = plan
             room = plan.room
+            n, lock, header_at = room.bytes, room.lock, room.header
         if B != pB or len(table.shape) != 2:
             raise ValueError(f"lens must be [{pB}] and table [{pB}, n]")
         H, d, dtype, T, pages = heads.H, self.sizes[1], self.dtype, B * nq, table.shape[1]
@@ -634,16 +655,17 @@ class PagedCache:
             ys = _rows("Y", Y, H, d, dtype, T)
         L = Q.new_empty((T, H), dtype=torch.float32) if lse else None
         stream = torch._C._cuda_getCurrentRawStream(at)
-        call = (_lib or lib()).avq_cache_attend_scratch
-        args = (heads, self.desc, Q.data_ptr(), qs, table.data_ptr(), pages, lens.data_ptr(), B, nq, Y.data_ptr(), ys,
-                L.data_ptr() if lse else None, header.data_ptr())
-        if room is None:
-            scratch = header.new_empty(n - 256)
-            st = call(*args, scratch.data_ptr(), n - 256, stream)
-        else:
-            with room.lock:
+        with lock:
+            if room is None:
+                kept = header.new_empty(n)
+                scratch = kept.data_ptr()
+            elif room.stream == stream and not _capturing():
+                scratch = room.rest
+            else:
                 scratch, kept = room.scratch(stream)
-                st = call(*args, scratch, room.bytes, stream)
+            st = (_lib or lib()).avq_cache_attend_scratch(
+                heads, self.desc, Q.data_ptr(), qs, table.data_ptr(), pages, lens.data_ptr(), B, nq, Y.data_ptr(), ys,
+                L.data_ptr() if lse else None, header_at, scratch, n, stream)
         if st != 0:
             raise AvqError(st, "avq_cache_attend")
         return (Y, L) if lse else Y

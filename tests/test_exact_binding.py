@@ -93,3 +93,17 @@ def test_header_and_scratch_apart_are_refused_where_unusable(lib):
         h, c, OK, 256, OK, 4, OK, 3, 1, Y, 256, 0, header, scratch, n, 0)
     assert call(header=0) == 5 and call(scratch=0) == 5 and call(n=n - 1) == 5 and call(header=0x1010) == 4
     assert call(scratch=0x1010) == 4 and call(Y=0) == 1
+
+
+def test_plans_can_be_copied():
+    import copy
+    import pickle
+    a = binding.ExactAttention(6, 2, 128, scale=0.3, causal=False, flags=binding.FLAG_SIMT, device="cpu", split=False)
+    b = binding.ExactAttention(6, 2, 64, device="cpu")
+    for x in (a, b):
+        for y in (copy.deepcopy(x), pickle.loads(pickle.dumps(x))):
+            assert [getattr(y.heads, f) for f, _ in binding.AvqHeads._fields_] == [getattr(x.heads, f) for f, _ in binding.AvqHeads._fields_]
+            assert y.dtype is x.dtype and y.room.bytes == x.room.bytes and y.room.header == y.workspace.data_ptr() != x.room.header
+    p = _cached()[0].plan(4, 2, flags=binding.FLAG_SIMT)
+    q = copy.deepcopy(p)
+    assert q[2:] == p[2:] and q[0].flags == p[0].flags and q.room.header == q[1].data_ptr() != p.room.header and q[1].numel() == p[1].numel()
