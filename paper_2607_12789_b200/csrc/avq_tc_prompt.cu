@@ -55,12 +55,32 @@ struct Shared {
   uint64_t task_full[kTasks], task_free[kTasks], drained;
   Task task[kTasks];
   uint32_t tmem;
+  int progress;                  // tiles that have been asked for
   int abort_flag, wide[kTasks];
   int32_t before[kMostSplit + 1];   // split calls: tiles of keys, with the setups, of the pieces before each
 };
 
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// As mbar_wait, but the limit is on the time without progress: some waits last a whole task (value tiles that the guards see
+// first, room for the next task), which may be millions of tiles.  Ends all the same: there are only so many tiles.
+__device__ __forceinline__ bool mbar_wait_or_progress(uint64_t* bar, uint32_t parity, volatile int* abort_flag, const volatile int* progress,
+                                                      int32_t* status_word, int32_t code) {
+  if (mbar_test_wait(bar, parity)) return true;
+  while (true) {
+    const int seen = *progress;
+    const unsigned long long t0 = global_timer_ns();
+    for (uint32_t polls = 0; polls < kWaitLimitPolls; ++polls) {
+      if (mbar_try_wait(bar, parity, kWaitTryNs)) return true;
+      if (*abort_flag) return false;
+      if (global_timer_ns() - t0 > kWaitLimitNs) break;
+    }
+    if (*progress == seen) break;
+  }
+  *abort_flag = 1;
+  if (status_word) atomicCAS(status_word, 0, code);
+  return false;
 }
 // 32 columns of this thread's row; the registers are not valid before tmem_wait.
 __device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t (&r)[32]) {
@@ -244,7 +264,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     }
     for (int i = 0; i < kTasks; ++i) { mbar_init(&sh.task_full[i], 1); mbar_init(&sh.task_free[i], kThreads / 32 - 1); }
     mbar_init(&sh.drained, 1);
-    sh.abort_flag = 0;
+    sh.abort_flag = sh.progress = 0;
     mbar_fence_init();
   }
   // rows of a tile that hold no query: whatever was in shared memory might be NaN and slow the softmax down
@@ -258,7 +278,10 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   tc_fence_after();
   const uint32_t tmem = sh.tmem;
   volatile int* abort_flag = &sh.abort_flag;
-  auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, a.status, DEV_TIMEOUT_ATTEND); };
+  volatile int* progress = &sh.progress;
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    return mbar_wait_or_progress(bar, parity, abort_flag, progress, a.status, DEV_TIMEOUT_ATTEND);
+  };
   auto wait_warp = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
   // The task number t, for all roles but the one that hands them out; false: no more (or the CTA gave up).
   auto next_task = [&](int t, Task& task) {
@@ -311,6 +334,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           uint64_t* bar = guard ? &sh.raw[g % kReady] : &sh.full[slot];
           if (guard) mbar_arrive(&sh.full[slot]);
           mbar_expect_tx(bar, tile_bytes<D>());
+          *progress = e;
           for (int s = 0; s < kSub; ++s)
             tma_load_3d(ring + slot * tile_bytes<D>() + s * kSubBytes, (x & 1) ? &tmV : &tmK, 64 * s, task.hk, task.piece.k0 + j * kTile, bar);
         }
