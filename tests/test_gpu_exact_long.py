@@ -1,13 +1,14 @@
-"""Exact attention at the far ends of its envelope: very many keys of one task."""
+"""Exact attention at the far ends of its envelope: very many keys of one task, very many sequences of one call."""
 import math
 
 import pytest
 import torch
 
 from paper_2607_12789_b200 import binding
+from tests import exact_reference as ref
 
 pytestmark = pytest.mark.gpu
-BF16 = torch.bfloat16
+F32, BF16 = torch.float32, torch.bfloat16
 
 
 def _ints(v):
@@ -34,3 +35,31 @@ def test_a_task_longer_than_the_limit_of_a_wait(causal):
     assert ((Y[0, 0].double() - want).abs() <= 2.0 ** -20 + half * want.abs()).all()
     assert abs(L.item() - math.log(n)) <= 2.0 ** -20 + 2.0 ** -23 * math.log(n)
 
+
+@pytest.mark.parametrize("dtype,flags,d", [(BF16, 0, 64), (BF16, 0, 128), (F32, 0, 64), (BF16, binding.FLAG_SIMT, 64)])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "all"])
+def test_thousands_of_sequences(dtype, flags, d, causal):
+    """4000 packed sequences of 0 to 20 tokens, padded for the reference to the longest."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(307)
+    S, most, H, Hk = 4000, 20, 4, 2
+    lens = [(7 * i) % (most + 1) for i in range(S)]
+    ends = [0]
+    for n in lens:
+        ends.append(ends[-1] + n)
+    T = ends[-1]
+    Q, K, V = (torch.randn(T, m, d, device="cuda", generator=g).to(dtype) for m in (H, Hk, Hk))
+    att = binding.ExactAttention(H, Hk, d, dtype=dtype, causal=causal, flags=flags)
+    Y, L = att(Q, K, V, _ints(ends), lse=True)
+    att.check()
+    at, i = torch.tensor(ends[:-1], device="cuda")[:, None], torch.arange(most, device="cuda")
+    there = i < torch.tensor(lens, device="cuda")[:, None]
+    rows = torch.where(there, at + i, torch.zeros_like(at))
+    pad = lambda x: x[rows].double().repeat_interleave(H // x.shape[1], 2)
+    s = att.heads.scale * torch.einsum("sihd,sjhd->shij", pad(Q), pad(K))
+    seen = there[:, None, None, :] & ((i <= i[:, None]) if causal else torch.ones(most, most, dtype=torch.bool, device="cuda"))
+    s = s.masked_fill(~seen, -math.inf)
+    y = torch.einsum("shij,sjhd->sihd", torch.softmax(s, -1).nan_to_num(0.0), pad(V))
+    l = torch.logsumexp(s, -1).transpose(1, 2)
+    ty, tl = ref.tolerance(d, most, dtype, ref.most_logit(Q, K, att.heads.scale), V.abs().max().item(), not flags)
+    ref.check(Y, L, y[there], l[there], ty, tl)
