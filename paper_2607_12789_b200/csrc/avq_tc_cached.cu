@@ -457,7 +457,8 @@ struct Warp {
             for (int e = 0; e < 4; ++e) {
               const float f = __uint_as_float(h[e]), fh = tf32_high(f);
               h[e] = __float_as_uint(fh);
-              x[e] = tf32_low(f, fh);
+              // (weights go up to 2^8: two of an infinity's stand-ins can overflow, and then have to have its sign)
+              x[e] = tf32_low(f, fh) | (__float_as_uint(f) & 0x80000000u);
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {

@@ -162,3 +162,26 @@ def test_an_infinite_query_element(d, inf):
             c.append(k, V, torch.arange(n, dtype=torch.int32, device="cuda"))
             y, l = c.attend(Q[40:41], _ints([[0, 1, 2, 3]]), _ints([n]), lse=True, flags=flags)
             assert (y == 0).all() and (l == -math.inf).all() if ok else torch.isnan(y).all()
+
+
+def _few(n, d, H, logits):
+    """Queries whose logits over n keys are the given ones (a scale of 1/8), values of 1."""
+    Q, K = torch.zeros(1, H, d, device="cuda"), torch.zeros(n, H, d, device="cuda")
+    Q[:, :, 0], K[:, :, 0] = 1.0, 8 * torch.tensor(logits, device="cuda")[:, None]
+    return Q, K, torch.ones(n, H, d, device="cuda")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("inf", [math.inf, -math.inf])
+@pytest.mark.parametrize("flags", [0, SIMT], ids=["tc", "simt"])
+def test_several_infinite_values_of_large_weights(d, inf, flags):
+    """Logits of 0 first, then logits that make weights of nearly 2^8 relative to those: values of the same infinity add up to it."""
+    n, H = 128, 2
+    Q, K, V = _few(n, d, H, [0.0] * 64 + [7.9 * math.log(2)] * 64)
+    V[70:74, :, 5] = inf
+    c = binding.PagedCache.empty(n // 16, 16, H, d, dtype=F32)
+    c.append(K, V, torch.arange(n, dtype=torch.int32, device="cuda"))
+    y = c.attend(Q, torch.arange(n // 16, dtype=torch.int32, device="cuda")[None], _ints([n]), scale=0.125, flags=flags)
+    assert (y[0, :, 5] == inf).all()
+    y[:, :, 5] = 1.0
+    assert ((y - 1).abs() <= 1e-5).all()
