@@ -110,9 +110,11 @@ __device__ __forceinline__ float tf32_high(float x) { return __uint_as_float(__f
 // NaN.  (The product of an infinity and a low part of zero is NaN all the same, and that of the number and a factor above 340
 // is an infinity of the other sign, perhaps: logits that are NaN are taken again from the operands themselves.)
 __device__ __forceinline__ uint32_t tf32_low(float x, float h) { return __float_as_uint(fminf(x - h, 1e36f)) + 0x1000u; }
-// The same of a weight, never zero beside a high part: 2^-30 of it at least, so that an infinite value times it is that
-// infinity and no NaN.
-__device__ __forceinline__ uint32_t tf32_low_weight(float p, float h) { return __float_as_uint(fmaxf(p - h, h * 9.3132257e-10f)) + 0x1000u; }
+// The same of a weight, never zero beside a high part, so that an infinite value times it is that infinity and no NaN: 2^-30 of
+// it at least, and 2^-126, which is the smallest that a weight is (smaller ones are zero).
+__device__ __forceinline__ uint32_t tf32_low_weight(float p, float h) {
+  return __float_as_uint(fmaxf(fmaxf(p - h, h * 9.3132257e-10f), fminf(p, 1.17549435e-38f))) + 0x1000u;
+}
 __device__ __forceinline__ float low_f(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float high_f(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
 // Three bfloat16 parts of a pair of float32 values, which add up to them exactly (but for values near the smallest).

@@ -185,3 +185,25 @@ def test_several_infinite_values_of_large_weights(d, inf, flags):
     assert (y[0, :, 5] == inf).all()
     y[:, :, 5] = 1.0
     assert ((y - 1).abs() <= 1e-5).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("inf", [math.inf, -math.inf])
+@pytest.mark.parametrize("flags", [0, SIMT], ids=["tc", "simt"])
+@pytest.mark.parametrize("powers", [range(-104, -96), range(-112, -104), range(-120, -112), range(-125, -120)])
+def test_an_infinite_value_of_a_tiny_weight(d, inf, flags, powers):
+    """A weight near the smallest of float32 (2^-126) is one all the same, powers of two among them: an infinity under it
+    reaches the row."""
+    n = 64
+    H = len(powers)
+    Q, K, V = torch.zeros(1, H, d, device="cuda"), torch.zeros(n, H, d, device="cuda"), torch.ones(n, H, d, device="cuda")
+    Q[:, :, 0], K[40, :, 0] = 1.0, torch.tensor(powers, device="cuda").float()
+    V[40, :, 5] = inf
+    c = binding.PagedCache.empty(n // 16, 16, H, d, dtype=F32)
+    c.append(K, V, torch.arange(n, dtype=torch.int32, device="cuda"))
+    att = binding.ExactAttention(H, H, d, dtype=F32, scale=math.log(2), causal=False, flags=flags)
+    for y in (att(Q, K, V, _ints([0, 1]), _ints([0, n])),
+              c.attend(Q, torch.arange(n // 16, dtype=torch.int32, device="cuda")[None], _ints([n]), scale=math.log(2), flags=flags)):
+        assert (y[0, :, 5] == inf).all()
+        y[:, :, 5] = 1.0
+        assert ((y - 1).abs() <= 1e-5).all()
