@@ -207,3 +207,33 @@ def test_an_infinite_value_of_a_tiny_weight(d, inf, flags, powers):
         assert (y[0, :, 5] == inf).all()
         y[:, :, 5] = 1.0
         assert ((y - 1).abs() <= 1e-5).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("inf", [math.inf, -math.inf])
+@pytest.mark.parametrize("flags", [0, SIMT], ids=["tc", "simt"])
+@pytest.mark.parametrize("n", [150, 2500])
+def test_one_infinite_element_of_a_bfloat16_key(d, inf, flags, n):
+    """Prompts (the longer one split along its keys) and a cache, the last 40 queries."""
+    g = _gen(109 + d)
+    nq, H, Hk, dim, BF16 = 40, 4, 2, 37, torch.bfloat16
+    Q, K, V = _factors("exact", g, nq, H, d, dim), _randn(g, n, Hk, d), _randn(g, n, Hk, d)
+    K[:, :, dim] = 0.0
+    K[3, 0, dim] = K[n // 2, 1, dim] = K[n - 2, 0, dim] = inf
+    Q, K, V = Q.to(BF16), K.to(BF16), V.to(BF16)
+    att = binding.ExactAttention(H, Hk, d, flags=flags)
+    c = binding.PagedCache.empty(-(-n // 16), 16, Hk, d)
+    c.append(K, V, torch.arange(n, dtype=torch.int32, device="cuda"))
+    table = torch.arange(-(-n // 16), dtype=torch.int32, device="cuda")[None]
+    plan = c.plan(H, 1, nq, flags=flags)
+    for Y, L in (att(Q, K, V, _ints([0, nq]), _ints([0, n]), lse=True), c.attend(Q, table, _ints([n]), lse=True, plan=plan)):
+        some = 0
+        for h in range(H):
+            ok, y, l, _, _ = _expect(Q[:, h], K[:, h // 2], V[:, h // 2], [n - nq + 1 + i for i in range(nq)], att.heads.scale, d)
+            finite = torch.where(torch.isfinite(K), K, torch.zeros_like(K))
+            ty, tl = ref.tolerance(d, n, BF16, ref.most_logit(Q, finite, att.heads.scale), V.abs().max().item(), not flags)
+            some += int(ok.sum())
+            _compare(Y[:, h], L[:, h], ok, y, l, ty, tl)
+        assert some > 40
+    att.check()
+    c.check(plan)
