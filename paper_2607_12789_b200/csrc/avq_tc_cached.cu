@@ -284,6 +284,7 @@ struct Warp {
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[n][e] *= qback[n][e & 1];
     } else {
+      float low[NT][4] = {};                               // sums of the products with a low part
 #pragma unroll 4
       for (int c = 0; c < D / 16; ++c) {
         const uint4 u = lds128(at + g * (4 * D) + 16 * ((4 * c + t) ^ swizzle(g)));
@@ -301,12 +302,16 @@ struct Warp {
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
             const uint4 f = shared[((2 * c + k) * NT + n) * 32 + lane];
-            mma_tf32(s[n], lo, f.x, f.y);
-            mma_tf32(s[n], hi, f.z, f.w);
+            mma_tf32(low[n], lo, f.x, f.y);
+            mma_tf32(low[n], hi, f.z, f.w);
             mma_tf32(s[n], hi, f.x, f.y);
           }
         }
       }
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[n][e] += low[n][e];
     }
   }
 
