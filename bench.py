@@ -72,7 +72,7 @@ def peaks():
 
 def measured_traffic(workload: str, kernel: str):
     """DRAM bytes per launch of a stage's kernels from the last ncu capture, or None when the capture was
-    taken from other kernel sources than the ones this run was built from."""
+    taken from other sources of those kernels than the ones this run was built from."""
     path = os.path.join(ROOT, "profiles", "ncu_traffic.json")
     if not os.path.exists(path):
         return None, "no capture recorded"

@@ -33,16 +33,27 @@ def _nvcc() -> str:
     return exe
 
 
-def source_hash() -> str:
-    """Short digest of every kernel source and header the library is built from: identifies which
-    sources a profiler capture (or any other stored measurement) belongs to."""
+FORWARD_SOURCES = ("avq_tc_assign.cu", "avq_tc_aggregate.cu", "avq_tc_attend.cu")
+
+
+def source_hash(sources=FORWARD_SOURCES) -> str:
+    """Short digest of kernel sources and of the headers in csrc/ that they include, directly or not: identifies which
+    kernels a profiler capture (or any other stored measurement) belongs to.  The default: those of the quantized forward on the
+    tensor cores, which the captures are of.  (The public header declares the entry points; kernel code is not in it.)"""
     import hashlib
+    import re
+    files, todo = set(), list(sources)
+    while todo:
+        name = todo.pop()
+        path = os.path.join(CSRC, name)
+        if name in files or not os.path.exists(path):
+            continue
+        files.add(name)
+        todo += re.findall(r'^\s*#include "([^"]+)"', open(path).read(), re.M)
     h = hashlib.sha256()
-    files = [os.path.join(ROOT, "include", "avq_attn.h")]
-    files += sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cu", ".cuh", ".h")))
-    for path in files:
-        h.update(os.path.basename(path).encode())
-        h.update(open(path, "rb").read())
+    for name in sorted(files):
+        h.update(name.encode())
+        h.update(open(os.path.join(CSRC, name), "rb").read())
     return h.hexdigest()[:16]
 
 
