@@ -1,4 +1,5 @@
-"""Exact attention at the far ends of its envelope: very many keys of one task, very many sequences of one call."""
+"""Exact attention at the far ends of its envelope: very many keys of one task, very many sequences of one call,
+very many query heads to a key head."""
 import math
 
 import pytest
@@ -63,3 +64,32 @@ def test_thousands_of_sequences(dtype, flags, d, causal):
     l = torch.logsumexp(s, -1).transpose(1, 2)
     ty, tl = ref.tolerance(d, most, dtype, ref.most_logit(Q, K, att.heads.scale), V.abs().max().item(), not flags)
     ref.check(Y, L, y[there], l[there], ty, tl)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 64), (BF16, 128), (F32, 64)])
+@pytest.mark.parametrize("G", [43, 65, 100, 128])
+@pytest.mark.parametrize("lq,lk", [([3, 0, 20], [3, 0, 20]), ([1, 7], [2100, 300])], ids=["short", "split"])
+def test_many_query_heads_to_a_key_head(dtype, d, G, lq, lk):
+    """Tiles of a few queries, some of whose rows stay empty; the same queries over a cache, in blocks of 16 rows."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(311)
+    Hk, page = 2, 16
+    H = G * Hk
+    ends = lambda lens: [sum(lens[:i]) for i in range(len(lens) + 1)]
+    cq, ck = ends(lq), ends(lk)
+    Q, K, V = (torch.randn(n, m, d, device="cuda", generator=g).to(dtype) for n, m in ((sum(lq), H), (sum(lk), Hk), (sum(lk), Hk)))
+    att = binding.ExactAttention(H, Hk, d, dtype=dtype)
+    Y, L = att(Q, K, V, _ints(cq), _ints(ck), lse=True)
+    att.check()
+    rY, rL = ref.prompt(Q, K, V, cq, ck, True, att.heads.scale)
+    ty, tl = ref.tolerance(d, max(lk), dtype, ref.most_logit(Q, K, att.heads.scale), V.abs().max().item(), True)
+    ref.check(Y, L, rY, rL, ty, tl)
+    b = max(range(len(lk)), key=lambda i: lk[i])            # the longest sequence, its queries the newest of its keys
+    n, nq, pages = lk[b], lq[b], -(-lk[b] // page)
+    c = binding.PagedCache.empty(pages, page, Hk, d, dtype=dtype)
+    c.append(K[ck[b]:ck[b + 1]], V[ck[b]:ck[b + 1]], torch.arange(n, dtype=torch.int32, device="cuda"))
+    plan = c.plan(H, 1, nq)
+    rows = slice(cq[b], cq[b + 1])
+    Y, L = c.attend(Q[rows], torch.arange(pages, dtype=torch.int32, device="cuda")[None], _ints([n]), lse=True, plan=plan)
+    c.check(plan)
+    ref.check(Y, L, rY[rows], rL[rows], ty, tl)
