@@ -97,6 +97,13 @@ __device__ __forceinline__ uint32_t centred(uint32_t pair) {
   asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(pair), "r"(0xc308c308u));   // - 136
   return r;
 }
+// c - 8 of the codes at bits 4 (i - i % 2) of both halves, 16 (c - 8) of those at bits 4 i (odd i), as halves, exactly
+__device__ __forceinline__ uint32_t centred_codes(uint32_t w, int i) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(w >> (8 * (i >> 1))), "r"((i & 1) ? 0x00f000f0u : 0x000f000fu), "r"(0x64006400u));
+  asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(r) : "r"((i & 1) ? 0x64806480u : 0x64086408u));   // 1024 and the middle
+  return r;
+}
 // c 2^-24 of the codes at bits 4 (i - i % 2) of both halves, c 2^-20 of those at bits 4 i (odd i)
 __device__ __forceinline__ uint32_t subnormal_codes(uint32_t w, int i) { return (w >> (8 * (i >> 1))) & ((i & 1) ? 0x00f000f0u : 0x000f000fu); }
 __device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either is

@@ -176,7 +176,7 @@ struct Warp {
         // the power of two that brings the row's largest element to 2^14 .. 2^15 (an infinity stays one)
         const int e = min(max((int)(__float_as_uint(most) >> 23), 27), 244);
         const float up = __uint_as_float((uint32_t)(268 - e) << 23);          // 2^(141 - e), e biased
-        const float back = __uint_as_float((uint32_t)(e + 10) << 23);        // 2^(e - 141 + 24)
+        const float back = __uint_as_float((uint32_t)(e + (PARTS == 1 ? 10 : -14)) << 23);   // 2^(e - 141), with 2^24 where codes are c 2^-24
 #pragma unroll
         for (int w = 0; w < kGroups; ++w)
 #pragma unroll
@@ -250,26 +250,45 @@ struct Warp {
 #pragma unroll
       for (int w = 0; w < kGroups; ++w) {
         float c[NT][4];
+        if constexpr (PARTS == 1) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const uint32_t f[4] = {subnormal_codes(x[w], 2 * k), subnormal_codes(y[w], 2 * k), subnormal_codes(x[w], 2 * k + 1),
-                                 subnormal_codes(y[w], 2 * k + 1)};
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t f[4] = {subnormal_codes(x[w], 2 * k), subnormal_codes(y[w], 2 * k), subnormal_codes(x[w], 2 * k + 1),
+                                   subnormal_codes(y[w], 2 * k + 1)};
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            if constexpr (PARTS == 1) {
+            for (int n = 0; n < NT; ++n) {
               if (k == 0) mma_f16_first(c[n], f, q[2 * w][n][0], q[2 * w][n][1]);
               else mma_f16(c[n], f, q[2 * w + 1][n][0], q[2 * w + 1][n][1]);
-            } else {
-              const uint2* from = reinterpret_cast<const uint2*>(shared) + ((2 * w + k) * NT + n) * 3 * 32 + lane;
-#pragma unroll
-              for (int i = 2; i >= 0; --i) {
-                if (k == 0 && i == 2) mma_f16_first(c[n], f, from[32 * i].x, from[32 * i].y);
-                else mma_f16(c[n], f, from[32 * i].x, from[32 * i].y);
-              }
             }
           }
+        } else {
+          // (codes about their middle, the high parts' products from zero, the others in a sum of their own: what the tensor cores
+          // cut off is little.  All in one chain, of codes from 0: up to 3e-6 of the result instead of 5e-7.)
+          float low[NT][4];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t f[4] = {centred_codes(x[w], 2 * k), centred_codes(y[w], 2 * k), centred_codes(x[w], 2 * k + 1),
+                                   centred_codes(y[w], 2 * k + 1)};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              const uint2* from = reinterpret_cast<const uint2*>(shared) + ((2 * w + k) * NT + n) * 3 * 32 + lane;
+              float high[4];
+              if (k == 0) mma_f16_first(low[n], f, from[64].x, from[64].y);
+              else mma_f16(low[n], f, from[64].x, from[64].y);
+              mma_f16(low[n], f, from[32].x, from[32].y);
+              mma_f16_first(high, f, from[0].x, from[0].y);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) c[n][e] = k == 0 ? high[e] : c[n][e] + high[e];
+            }
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c[n][e] += low[n][e];
         }
-        const float sx = high_f(px[w]), sy = high_f(py[w]), lx = low_f(px[w]), ly = low_f(py[w]);
+        const float sx = high_f(px[w]), sy = high_f(py[w]);
+        // (of a code's middle, where it is left out of the codes)
+        const float lx = PARTS == 1 ? low_f(px[w]) : fmaf(8.f, sx, low_f(px[w])), ly = PARTS == 1 ? low_f(py[w]) : fmaf(8.f, sy, low_f(py[w]));
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
