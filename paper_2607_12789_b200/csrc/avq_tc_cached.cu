@@ -303,29 +303,41 @@ struct Warp {
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[n][e] *= qback[n][e & 1];
     } else {
-      float low[NT][4] = {};                               // sums of the products with a low part
-#pragma unroll 4
-      for (int c = 0; c < D / 16; ++c) {
-        const uint4 u = lds128(at + g * (4 * D) + 16 * ((4 * c + t) ^ swizzle(g)));
-        const uint4 v = lds128(at + (g + 8) * (4 * D) + 16 * ((4 * c + t) ^ swizzle(g)));
-        const uint32_t xs[4] = {u.x, u.y, u.z, u.w}, ys[4] = {v.x, v.y, v.z, v.w};
+      // (sums of the products with a low part apart, those of the high parts from zero every 32 dimensions and added in
+      // registers: the tensor cores cut sums off)
+      float low[NT][4] = {};
+#pragma unroll 2
+      for (int c2 = 0; c2 < D / 32; ++c2) {
+        float high[NT][4];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          uint32_t hi[4] = {xs[2 * k], ys[2 * k], xs[2 * k + 1], ys[2 * k + 1]}, lo[4];
+        for (int c1 = 0; c1 < 2; ++c1) {
+          const int c = 2 * c2 + c1;
+          const uint4 u = lds128(at + g * (4 * D) + 16 * ((4 * c + t) ^ swizzle(g)));
+          const uint4 v = lds128(at + (g + 8) * (4 * D) + 16 * ((4 * c + t) ^ swizzle(g)));
+          const uint32_t xs[4] = {u.x, u.y, u.z, u.w}, ys[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float x = __uint_as_float(hi[i]), h = tf32_high(x);
-            hi[i] = __float_as_uint(h);
-            lo[i] = tf32_low(x, h);
-          }
+          for (int k = 0; k < 2; ++k) {
+            uint32_t hi[4] = {xs[2 * k], ys[2 * k], xs[2 * k + 1], ys[2 * k + 1]}, lo[4];
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            const uint4 f = shared[((2 * c + k) * NT + n) * 32 + lane];
-            mma_tf32(low[n], lo, f.x, f.y);
-            mma_tf32(low[n], hi, f.z, f.w);
-            mma_tf32(s[n], hi, f.x, f.y);
+            for (int i = 0; i < 4; ++i) {
+              const float x = __uint_as_float(hi[i]), h = tf32_high(x);
+              hi[i] = __float_as_uint(h);
+              lo[i] = tf32_low(x, h);
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              const uint4 f = shared[((2 * c + k) * NT + n) * 32 + lane];
+              mma_tf32(low[n], lo, f.x, f.y);
+              mma_tf32(low[n], hi, f.z, f.w);
+              if (c1 == 0 && k == 0) mma_tf32_first(high[n], hi, f.x, f.y);
+              else mma_tf32(high[n], hi, f.x, f.y);
+            }
           }
         }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[n][e] += high[n][e];
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n)
