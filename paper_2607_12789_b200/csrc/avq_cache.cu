@@ -2,7 +2,7 @@
 // rows out.  Both kernels are copies with a little arithmetic: a lane takes 8 dimensions (16 or 32
 // bytes) of a row, d/8 neighbouring lanes a row, so that a row's partner dimensions of the rotation and the groups of 32
 // of the 4-bit form are within a warp, and every lane has loaded its part before any stores (queries may be rotated in
-// place).  16384 tokens, 16 query and 8 key heads, d 128, bfloat16: into 4 bits with the rotation 60 us (216 MB, 3.6 TB/s, two
+// place).  16384 tokens, 16 query and 8 key heads, d 128, bfloat16: into 4 bits with the rotation 60 us (231 MB, 3.8 TB/s, two
 // thirds of the issue slots: the rotation's products and the codes are what is left), back 20 us (88 MB, 4.4 TB/s).
 #include "avq_exact.cuh"
 

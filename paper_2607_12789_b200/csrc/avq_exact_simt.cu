@@ -358,8 +358,9 @@ __global__ void __launch_bounds__(kCachedThreads) cached_simt_kernel(const Cache
 // otherwise the partial rows of CTAs c0 .. c1 are brought to their common maximum and added, each warp a share of them in
 // ascending order, the warps' sums in the order of the warps.
 // Threads of a row's CTA: two warps where segments are many (and parts of each few), eight where they are few (their parts
-// many).  64 and 256 threads: 512 segments 78.9 and 84.9 us with the kernel before, 24 segments 31.8 and 30.5, 8 segments 43.5
-// and 38.9.
+// many).  64 and 256 threads, with the kernel before, 4096 tokens of bfloat16 a segment: 8 segments 12.3 and 10.2 us, 24 13.6
+// and 13.0, 48 17.5 and 17.4, 64 28.6 and 28.8, 96 38.8 and 38.7, 128 49.9 and 51.4, 512 167 and 171; in 4 bits 13.1 and 11.1,
+// 15.7 and 15.0, 19.2 and 19.1, 21.5 and 21.5, 26.5 and 26.7, 31.8 and 34.1, 96 and 102.
 constexpr int kJoinMost = 256, kJoinFew = 64, kJoinMany = 128;
 template <typename T>
 __global__ void __launch_bounds__(kJoinMost) join_kernel(const CachedArgs a) {

@@ -22,15 +22,18 @@
 //   rounding of the weights meets c - 8 and not c.  The weights p step_g have a range of their own and stay bfloat16; an
 //   AND-OR makes 0x4300 | c, which is 128 + c, of a code, and a product of the same rounded weights with a constant -136
 //   takes the 136 out again.  (With three parts the 136 is taken off the codes: 143 times a part would cost the sum bits.)
-// float32: rows by tf32 products of two parts each (the lowest product left out: 2^-22 of a term; a unit's values are
-// summed from zero and added to the output in registers, since the tensor cores cut sums off); 4 bits with float32
-// queries by three parts of the query (half precision) and of the weight (bfloat16), which are all of their 24 bits.
+// float32: rows by tf32 products of two parts each (the lowest product left out: 2^-22 of a term; a unit's values and 32
+// dimensions of its logits are summed from zero and added in registers, the low parts' products apart, since the tensor cores
+// cut sums off; logits that the parts of an infinity make a NaN are taken again from the operands); 4 bits with float32
+// queries by three parts of the query (half precision) and of the weight (bfloat16), which are all of their 24 bits, with the
+// keys' codes about their middle too.
 //
 // Measured (B200, several calls one after another): 64 sequences of 1 .. 4096 tokens, 8 key heads, d 128, bfloat16 rows 78.5 us
 // for 467 MB, 5.95 TB/s, 91 % of the measured copy rate, the joining kernel in it; the same in 4 bits, lengths to 8192, with the
 // rows' way into the cache 91.7 us for 268 MB (2.9 TB/s), two sequences of 131072 and 28076 39 us for 102 MB: there the
 // instructions that take codes apart and scale (450 for 16 tokens of one head, half of the issue slots) and the start of the
-// CTAs are the time; float32 rows 31 us for 105 MB.
+// CTAs are the time; float32 rows 29.5 us for 105 MB, a captured call; 4 bits with float32 queries, 64 sequences of up to 4096
+// tokens, 8 key heads, d 128, 79 us.
 //
 // The running maximum of a row is raised only when a logit exceeds it by 2^8 (weights stay below 2^8, sums far inside
 // float32): most units need a vote instead of shuffles and rescaling.

@@ -13,13 +13,14 @@
 //   10, 11    clean the value tiles that not every row sees whole: rows behind the last key become zero (they are
 //             another sequence's), infinities and NaN too (a weight of zero times one of them would be NaN); the
 //             latter are added back at the end to the rows that do see them; warp 10 also hands out the tasks
-// Bound: per pair of tiles of 128 keys (d = 128) the products take 2048 cycles of the tensor pipe and the 32768
+// Bound at d = 128: per pair of tiles of 128 keys the products take 2048 cycles of the tensor pipe and the 32768
 // exponentials as many of the MUFU pipe, in turn for each tile of rows; what keeps them from overlapping fully is the way
 // from logits to weights and back.  A quarter of the exponentials by a polynomial on the FMA pipe was 4 % slower than
 // none (16384 tokens of 16 heads: 949 and 906 us): a second form of the code costs more than the pipe gains.
-// Measured: 16384 tokens, 16 heads on 4, d 128, causal 868 us (1267 TFLOP/s, 76 % of the measured burst rate; 1047 us and 1050
-// TFLOP/s when it runs on and on at the power limit), 16 prompts of up to 2048 tokens, 32 heads on 8, 182 us (710 TFLOP/s: a third
-// of the time is the first logits and the outputs of each of 1704 short pieces), d 64 620 TFLOP/s (bound by the exponentials).
+// Measured: 16384 tokens, 16 heads on 4, d 128, causal 886 us (1241 TFLOP/s, 75 % of the measured burst rate; 1035 us and 1062
+// TFLOP/s when it runs on and on at the power limit), 16 prompts of up to 2048 tokens, 32 heads on 8, 187 us (691 TFLOP/s: a third
+// of the time is the first logits and the outputs of each of 1704 short pieces).  d 64: half the products for as many exponentials,
+// which alone would allow 1190 TFLOP/s; 16384 tokens of 16 heads 706 (the way from logits to weights and back, again).
 // The maximum that weights refer to is raised only when a row exceeds it by 2^8, which spares nearly every rescaling of
 // O: weights stay below 2^8, and what they are relative to cancels in O / l.
 #include "avq_exact.cuh"
@@ -792,7 +793,12 @@ avq_status launch(const PromptArgs& a, cudaStream_t st) {
   sms = sms < kPromptCtas ? sms : kPromptCtas;
   const int64_t pieces = most_pieces(a.Tq, a.S, 2 * per), all = pieces * a.Hk;
   if (all >= (int64_t)1 << 30) return AVQ_ERR_UNSUPPORTED;
-  // Pieces that cannot fill the GPU, over keys that can be long, are split, if the caller's workspace holds the parts.
+  // Pieces that cannot fill the GPU, over keys that can be long, are split, if the caller's workspace holds the parts.  The host
+  // knows how many keys there are, not how they are spread.  64 queries a sequence, 4 heads to a key head, d 128, whole and split:
+  // one sequence of 1024, 2048, 16384 keys, 4 key heads 23.6 and 23.6, 37.9 and 25.1, 237 and 32.5 us; 4 sequences (36 pieces) of
+  // 512, 1024, 4096 keys 16.4 and 24.6, 23.6 and 26.4, 66.6 and 28.6; 8 key heads and 8 sequences (136 pieces) of 512, 2048, 8192
+  // keys 17.9 and 35.8, 39.7 and 51.3, 129 and 97; 16 sequences (264 pieces, not split) of 4096 keys 75.8 and 128.  So even
+  // short sequences lose up to some 30 us by the rule, and one long one among them gains hundreds.
   const bool split = a.parts && all <= kSplitBelow && pieces <= kMostSplit && a.S <= kMostSplit && a.Tk >= kSplitKeys;
   const int grid = split ? sms : (int)(all < sms ? all : sms), least = split ? kLeastTiles : 0;
   prompt_tc_kernel<D><<<grid, kThreads, prompt_smem<D>(), st>>>(tmQ, tmK, tmV, a, (int)pieces, least, a.parts);

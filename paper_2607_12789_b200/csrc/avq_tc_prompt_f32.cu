@@ -8,8 +8,10 @@
 // the next product's sum, key 2 t + 1 index t + 4.  The next tile's copies (cp.async) run under the products.
 // Bound by the products, three of each, whose sums the tensor cores cut off instead of rounding: the low parts' products have
 // sums of their own in Q K^T, a tile's P V is summed from zero and added in registers (all in one chain: 6.7e-6 of the result
-// off instead of 5.9e-7; only the first of the two left out: 1.1e-6).  Eight images of 785 tokens, 12 heads, d 64: 366 us, of
-// the CUDA cores 540; with one row tile to a warp 367, with three CTAs to an SM, whose registers do not hold the sums, 387.
+// off instead of 5.9e-7; only the first of the two left out: 1.1e-6).  Eight images of 785 tokens, 12 heads, d 64: 372 us, of
+// the CUDA cores 540; with one row tile to a warp as much, with three CTAs to an SM, whose registers do not hold the sums, 20 more.
+// 5 of it are for infinities: logits that their parts make a NaN are taken again from the rows (one branch for a tile: one for each
+// row of it cost 29), and the low part of a weight is never zero.
 #include "avq_exact_mma.cuh"
 
 namespace avq {
